@@ -63,9 +63,27 @@ typedef struct {
                            fewer: grouped-query attention, query head h reads K/V head
                            h / (num_heads / num_kv_heads)                                */
   int32_t head_dim;     /* 64, 128 or 256                                                */
-  int32_t dtype;        /* 0 = bf16                                                      */
-  int32_t layout;       /* 0 = the layout above                                          */
+  int32_t dtype;        /* IC_DTYPE_*                                                    */
+  int32_t layout;       /* 0 = the layout above (8-bit dtypes: the one below)            */
 } ic_pool_cfg;
+
+/*
+ * What the cache holds.  IC_DTYPE_E4M3 and IC_DTYPE_INT8 keep 8 bits a number: half the bytes per token (M) of bf16, and with them half
+ * the time of a decode row, half of a swap.  Queries, new keys and values, results and rows read back stay bf16.
+ *
+ * A vector x (one token's key, or value, of one head) is head_dim codes and one scale byte b:
+ *      a = max |x|,  e = the smallest integer >= -100 with a <= top * 2^e,  b = e + 127
+ *      code = x / 2^e rounded to nearest even,  value = code * 2^e
+ *   IC_DTYPE_E4M3  codes are e4m3 numbers (4 bits of significand, no infinities), top = 448
+ *   IC_DTYPE_INT8  codes are two's complement integers, top = 127
+ * A value is exact in bf16.  It is off from x by at most half a step: 2^-4 of |x| for e4m3 (for |x| >= 2^-6 * 2^e; below, 2^-10 * 2^e),
+ * 2^(e-1) for int8, which is less than a / 127 (e > -100).  (A finite a within half a step of the largest bf16 number may round to infinity.)
+ * A vector with a NaN or an infinity in it is kept as b = 255 and codes 0: all its values are NaN.
+ *
+ * Block of an 8-bit pool: codes [kv][kv_head][slot][dim], one byte each, then scale bytes [kv_head][kv][slot]; the block's size is
+ * rounded up to a multiple of 128 bytes (kv_block_bytes), the padding is never read.  The pool may start out with any contents.
+ */
+enum { IC_DTYPE_BF16 = 0, IC_DTYPE_E4M3 = 2, IC_DTYPE_INT8 = 3 };
 
 typedef struct ic_pool ic_pool; /* opaque; created by kv_pool_init, freed by kv_pool_destroy */
 
@@ -84,7 +102,8 @@ typedef struct ic_pool ic_pool; /* opaque; created by kv_pool_init, freed by kv_
 int kv_pool_init(const ic_pool_cfg* cfg, void* dev_pool_base, size_t pool_bytes, ic_pool** out);
 int kv_pool_destroy(ic_pool* pool); /* frees library-owned buffers; never the KV memory */
 
-/* block_size * 2 * num_kv_heads * head_dim * 2 bytes (K and V of one layer's block); 0 if pool is NULL. */
+/* K and V of one layer's block: block_size * 2 * num_kv_heads * head_dim * 2 bytes in a bf16 pool, block_size * 2 * num_kv_heads *
+ * (head_dim + 1) rounded up to 128 in an 8-bit pool; 0 if pool is NULL. */
 size_t kv_block_bytes(const ic_pool* pool);
 
 /* ------------------------------------------------------------------------------------------
@@ -137,16 +156,27 @@ int paged_attn_mixed(ic_pool* pool, const ic_batch_desc* desc, const void* dev_q
  * KV append (Section 4.2: a recomputation chunk joins the batch; Section 4.3: a partly recomputed
  * request continues in later iterations, so what one chunk computes must be in the cache for the
  * next).  Writes the keys and values computed for this iteration's query positions into the paged
- * cache: for every sequence s and row i < q_len[s], position t = ctx_len[s] - q_len[s] + i,
+ * cache (an 8-bit pool: quantised as they are written): for every sequence s and row i < q_len[s], position t = ctx_len[s] - q_len[s] + i,
  *      pool[block_tables[s][t / block_size]][K|V][h][t % block_size][:] = k_new|v_new[q_start[s] + i][h][:]
  * for decode sequences (q_len = 1: the new token) and chunks alike.  It is the step before
  * paged_attn_mixed on the same descriptor, on the same stream.  dev_k_new, dev_v_new: device bf16
- * [total_q_rows][num_kv_heads][head_dim]; rows no sequence owns are ignored.  Byte-exact; every
- * other slot of the cache keeps its bytes.  Two rows that address one slot (sequences sharing a
+ * [total_q_rows][num_kv_heads][head_dim]; rows no sequence owns are ignored.  Byte-exact (8-bit: the codes are exactly those of
+ * the definition above); every other slot of the cache keeps its bytes.  Two rows that address one slot (sequences sharing a
  * block they both write) give IC_EDUP; IC_FLAG_TRUSTED skips that check and the id checks.
  */
 int kv_write_span(ic_pool* pool, const ic_batch_desc* desc, const void* dev_k_new, const void* dev_v_new,
                   void* hip_stream);
+
+/*
+ * The other way round: reads cached positions back as bf16 rows.  For every sequence s and row i < q_len[s], position
+ * t = ctx_len[s] - q_len[s] + i,
+ *      k_out|v_out[q_start[s] + i][h][:] = the values at pool[block_tables[s][t / block_size]][K|V][h][t % block_size]
+ * q_len = ctx_len reads a whole context (to move it to a pool of another dtype: kv_read_span, then kv_write_span there, which keeps
+ * every value of an 8-bit cache).  dev_k_out, dev_v_out: device bf16 [total_q_rows][num_kv_heads][head_dim], not overlapping the pool
+ * or each other (IC_EINVAL); rows no sequence owns keep their bytes.  Exact: a bf16 cache's bytes, an 8-bit cache's values.  Sequences
+ * may share blocks.
+ */
+int kv_read_span(ic_pool* pool, const ic_batch_desc* desc, void* dev_k_out, void* dev_v_out, void* hip_stream);
 
 /*
  * Plan once, run for every layer.  One iteration's batch (Section 4.3) is the same for all layers of
@@ -167,6 +197,8 @@ int paged_attn_planned(ic_pool* pool, const ic_plan* plan, const void* dev_q, vo
  * plan's descriptor was not trusted and two of its rows address one cache slot. */
 int kv_write_span_planned(ic_pool* pool, const ic_plan* plan, const void* dev_k_new, const void* dev_v_new,
                           void* hip_stream);
+/* kv_read_span from the same plan. */
+int kv_read_span_planned(ic_pool* pool, const ic_plan* plan, void* dev_k_out, void* dev_v_out, void* hip_stream);
 int paged_attn_plan_destroy(ic_plan* plan);
 
 /* Host-only validation of a descriptor against a pool shape (what paged_attn_mixed checks when
@@ -191,7 +223,9 @@ typedef struct {
                                  one workgroup per work item when the items are short or split),
                                  1 = alone one workgroup per work item, 2 = persistent, 3 = persistent, alone too
                                  the slim builds that run beside the tile kernel (in a grouped-query pool of
-                                 head_dim 128 with groups of up to 16: the slim group kernel)  */
+                                 head_dim 128 with groups of up to 16: the slim group kernel).  8-bit pools have one
+                                 row kernel, one workgroup per work item: row_variant, row_launch and row_slots
+                                 have no effect there                                         */
   int32_t row_slots;          /* resident workgroups of the persistent row kernel (and of the slim group kernel);
                                  0 = one per CU */
   int32_t mfma_min_keys;      /* the softmax weights of query rows that see fewer keys than this are not rounded to
@@ -224,6 +258,9 @@ int ic_plan_query(const ic_pool* pool, const ic_batch_desc* desc, ic_plan_info* 
  * (few items, slot_merge and arrived: ic_plan_launches below).
  *   row item   (8 x int32): seq, qrow, k_begin, k_end, slot (-1: whole row, direct output), 0, 0, 0
  *              one query row against keys [k_begin, k_end) of its sequence, all heads
+ *              8-bit pools: seq, qrow, k_begin, k_end, slot, n_rows, pos0, nparts: n_rows consecutive query rows from qrow, the first at
+ *              position pos0, against keys [k_begin, k_end) cut at each row's own position; partial slot of row r: slot + r * nparts
+ *              (nparts 0: a decode row, n_rows 1)
  *   tile item  (8 x int32): seq, qrow0, n_rows, pos0, k_begin, k_end, slot0 (-1: direct), nparts
  *              n_rows consecutive query rows from qrow0, the first at position pos0, against keys
  *              [k_begin, k_end) cut at each row's own position; partial slot of row r: slot0 + r * nparts

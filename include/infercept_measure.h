@@ -20,8 +20,9 @@ extern "C" {
  * ic_prof_end synchronises the recorded events and returns totals per kernel kind.
  * ------------------------------------------------------------------------------------------ */
 enum { IC_K_ROW = 0, IC_K_TILE = 1, IC_K_MERGE = 2, IC_K_PACK = 3, IC_K_UNPACK = 4, IC_K_UPLOAD = 5, IC_K_APPEND = 6,
-       IC_K_GROUP = 7, IC_K_COUNT = 8 };
-/* IC_K_UPLOAD: the kernel that copies a call's descriptor from pinned host memory to the device. */
+       IC_K_GROUP = 7, IC_K_READ = 8, IC_K_COUNT = 9 };
+/* IC_K_UPLOAD: the kernel that copies a call's descriptor from pinned host memory to the device.  IC_K_GROUP: also the row kernel of
+ * an 8-bit pool.  IC_K_READ: kv_read_span. */
 typedef struct {
   int32_t launches[IC_K_COUNT];
   float total_ms[IC_K_COUNT];
@@ -69,7 +70,7 @@ int ic_hbm_ceiling(const void* dev_src, void* dev_dst, size_t bytes, int32_t mod
  * word.  *gbps = n * kv_block_bytes * reps bytes over the time of `reps` back-to-back launches.
  * host_ids: n block ids in [0, num_blocks), duplicates allowed; dev_sink: device, 16 bytes, may be
  * written.  Allocates and frees its own device copy of the id list.  Synchronous.
- * Errors: IC_ENULL, IC_EINVAL, IC_ERANGE, IC_EALIGN, IC_EHIP. */
+ * bf16 pools only.  Errors: IC_ENULL, IC_EINVAL, IC_ERANGE, IC_EALIGN, IC_EUNSUPPORTED, IC_EHIP. */
 int ic_paged_read_ceiling(const ic_pool* pool, const int32_t* host_ids, int32_t n, void* dev_sink,
                           int32_t reps, void* hip_stream, double* gbps);
 

@@ -20,8 +20,9 @@ IC_ENULL, IC_EINVAL, IC_ERANGE, IC_ESIZE, IC_EALIGN = -1, -2, -3, -4, -5
 IC_EDUP, IC_EUNSUPPORTED, IC_EOVERLAP, IC_EHIP, IC_ENOMEM, IC_ELIMIT = -6, -7, -8, -9, -10, -11
 IC_STATIC_PACK_MAX_BLOCKS = 65536
 IC_FLAG_TRUSTED = 1
-IC_K_ROW, IC_K_TILE, IC_K_MERGE, IC_K_PACK, IC_K_UNPACK, IC_K_UPLOAD, IC_K_APPEND, IC_K_GROUP, IC_K_COUNT = range(9)
-KERNEL_NAMES = ("row", "tile", "merge", "pack", "unpack", "upload", "append", "group")
+IC_DTYPE_BF16, IC_DTYPE_E4M3, IC_DTYPE_INT8 = 0, 2, 3
+IC_K_ROW, IC_K_TILE, IC_K_MERGE, IC_K_PACK, IC_K_UNPACK, IC_K_UPLOAD, IC_K_APPEND, IC_K_GROUP, IC_K_READ, IC_K_COUNT = range(10)
+KERNEL_NAMES = ("row", "tile", "merge", "pack", "unpack", "upload", "append", "group", "read")
 
 EXPORTS = (
     "ic_strerror", "kv_pool_init", "kv_pool_destroy", "kv_block_bytes",
@@ -35,7 +36,7 @@ EXPORTS = (
     "ic_chunk_tokens", "ic_chunk_count", "ic_saturation_point", "ic_schedule_intercepted",
     "paged_attn_plan_create", "paged_attn_planned", "paged_attn_plan_destroy", "kv_write_span_planned",
     "ic_mfma_ceiling", "ic_plan_image", "ic_hbm_ceiling", "ic_paged_read_ceiling", "kv_pack_blocks_static",
-    "ic_plan_launches",
+    "ic_plan_launches", "kv_read_span", "kv_read_span_planned",
 )
 IC_CEILING_OPERAND_BYTES = 1 << 20
 IC_CEILING_SINK_BYTES = 256 * 512 * 4 + 256 * 16
@@ -138,6 +139,8 @@ def lib():
         L.paged_attn_planned.argtypes = [vp, vp, vp, vp, vp]
         L.kv_write_span_planned.argtypes = [vp, vp, vp, vp, vp]
         L.paged_attn_plan_destroy.argtypes = [vp]
+        L.kv_read_span.argtypes = [vp, C.POINTER(BatchDesc), vp, vp, vp]
+        L.kv_read_span_planned.argtypes = [vp, vp, vp, vp, vp]
         L.ic_check_batch.argtypes = [C.POINTER(PoolCfg), C.POINTER(BatchDesc)]
         L.ic_pool_set_tuning.argtypes = [vp, C.POINTER(Tuning)]
         L.ic_plan_query.argtypes = [vp, C.POINTER(BatchDesc), C.POINTER(PlanInfo)]
@@ -202,6 +205,13 @@ def make_cfg(num_blocks, num_heads, head_dim, block_size=16, num_kv_heads=None, 
                    int(num_heads if num_kv_heads is None else num_kv_heads), int(head_dim), dtype, layout)
 
 
+def block_bytes(num_kv_heads, head_dim, block_size=16, dtype=IC_DTYPE_BF16) -> int:
+    """Bytes of one block (K and V) of a pool: what kv_block_bytes says of it."""
+    if dtype == IC_DTYPE_BF16:
+        return block_size * 2 * num_kv_heads * head_dim * 2
+    return -(-block_size * 2 * num_kv_heads * (head_dim + 1) // 128) * 128
+
+
 class HostDesc:
     """Keeps the numpy arrays of a batch descriptor alive next to the ctypes struct."""
 
@@ -241,13 +251,13 @@ class KvPool:
             raise InferceptError(rc, "kv_pool_init")
 
     @classmethod
-    def from_tensor(cls, pool_t, num_heads, head_dim, block_size=16, num_kv_heads=None):
+    def from_tensor(cls, pool_t, num_heads, head_dim, block_size=16, num_kv_heads=None, dtype=IC_DTYPE_BF16):
         """pool_t: a contiguous torch device tensor holding [blocks][2][Hkv][B][D] bf16 (Hkv = num_kv_heads,
-        num_heads if not given)."""
+        num_heads if not given), or with dtype IC_DTYPE_E4M3 or IC_DTYPE_INT8 [blocks][block_bytes(...)] bytes."""
         nbytes = pool_t.numel() * pool_t.element_size()
         hkv = num_heads if num_kv_heads is None else num_kv_heads
-        bb = block_size * 2 * hkv * head_dim * 2
-        obj = cls(make_cfg(nbytes // bb, num_heads, head_dim, block_size, hkv), pool_t.data_ptr(), nbytes)
+        bb = block_bytes(hkv, head_dim, block_size, dtype)
+        obj = cls(make_cfg(nbytes // bb, num_heads, head_dim, block_size, hkv, dtype), pool_t.data_ptr(), nbytes)
         obj._keep = pool_t
         return obj
 
@@ -364,6 +374,18 @@ class KvPool:
         rc = lib().kv_write_span(self._h, C.byref(desc.struct), C.c_void_p(k_ptr), C.c_void_p(v_ptr), C.c_void_p(stream))
         if check and rc != IC_OK:
             raise InferceptError(rc, "kv_write_span")
+        return int(rc)
+
+    def kv_read_span_planned(self, plan: "AttnPlan", k_ptr: int, v_ptr: int, stream: int = 0, check: bool = True) -> int:
+        rc = lib().kv_read_span_planned(self._h, plan._h, C.c_void_p(k_ptr), C.c_void_p(v_ptr), C.c_void_p(stream))
+        if check and rc != IC_OK:
+            raise InferceptError(rc, "kv_read_span_planned")
+        return int(rc)
+
+    def kv_read_span(self, desc: HostDesc, k_ptr: int, v_ptr: int, stream: int = 0, check: bool = True) -> int:
+        rc = lib().kv_read_span(self._h, C.byref(desc.struct), C.c_void_p(k_ptr), C.c_void_p(v_ptr), C.c_void_p(stream))
+        if check and rc != IC_OK:
+            raise InferceptError(rc, "kv_read_span")
         return int(rc)
 
     def kv_pack_blocks(self, ids, staging_ptr: int, staging_bytes: int, stream: int = 0, check: bool = True) -> int:

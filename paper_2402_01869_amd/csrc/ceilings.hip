@@ -93,6 +93,7 @@ extern "C" int ic_paged_read_ceiling(const ic_pool* pool, const int32_t* host_id
   if (!pool || !host_ids || !dev_sink || !gbps) return IC_ENULL;
   const PoolView pv = pool_view(pool);
   if (n < 1 || reps < 1 || reps > 10000 || (uint64_t)n * (uint64_t)pv.cfg.num_kv_heads > 0x7fffffffull) return IC_EINVAL;
+  if (pv.cfg.dtype != IC_DTYPE_BF16) return IC_EUNSUPPORTED;  // the probe reads bf16 tiles
   const int rc0 = ic_check_ids(&pv.cfg, host_ids, n, 0);
   if (rc0 != IC_OK) return rc0;
   if ((uintptr_t)dev_sink & 15) return IC_EALIGN;

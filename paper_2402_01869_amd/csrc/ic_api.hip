@@ -92,7 +92,7 @@ int check_cfg(const ic_pool_cfg* c) {
   if (c->num_blocks < 1 || c->num_heads < 1 || c->num_kv_heads < 1 || c->head_dim < 1 ||
       c->block_size < 1)
     return IC_EINVAL;
-  if (c->dtype != 0 || c->layout != 0) return IC_EUNSUPPORTED;
+  if ((c->dtype != IC_DTYPE_BF16 && c->dtype != IC_DTYPE_E4M3 && c->dtype != IC_DTYPE_INT8) || c->layout != 0) return IC_EUNSUPPORTED;
   if (c->block_size != kBlockSize) return IC_EUNSUPPORTED;
   if (c->num_kv_heads > c->num_heads || c->num_heads % c->num_kv_heads != 0) return IC_EINVAL;
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return IC_EUNSUPPORTED;
@@ -100,7 +100,10 @@ int check_cfg(const ic_pool_cfg* c) {
   return IC_OK;
 }
 
+bool is_q8(const ic_pool_cfg& c) { return c.dtype != IC_DTYPE_BF16; }
+
 size_t cfg_block_bytes(const ic_pool_cfg& c) {
+  if (is_q8(c)) return align_up((size_t)c.block_size * 2 * c.num_kv_heads * (c.head_dim + 1), 128);
   return (size_t)c.block_size * 2 * c.num_kv_heads * c.head_dim * 2;
 }
 
@@ -188,6 +191,9 @@ struct PlanSizes {
   int few_runs, few_rows;              // ... of which the last few_rows are the rows of few_runs few-key units (tile kernels)
                                        // and the others the vector kernel's
   int tile_g_shift;                    // log2 of the query heads one tile workgroup serves
+  bool q8;                             // an 8-bit pool: its row kernel takes all row items, several rows of a span to an item
+  int item_rows;                       // query rows of a row item, at most (1 in a bf16 pool)
+  int short_span;                      // spans of up to so many rows are row items (0 in a bf16 pool)
   bool spans_as_rows;
   bool few_as_units;                   // few-key rows of spans go to the tile kernels' few-key body
   bool decode_as_tiles;                // grouped pools, span_kernel = 2: decode rows as one-row tile items
@@ -230,8 +236,8 @@ struct SeqRoute {
 SeqRoute route(const PlanSizes& ps, int c, int n) {
   SeqRoute r;
   r.n_few = std::min(n, std::max(0, ps.min_keys - 1 - (c - n)));
-  r.rest_rows = n == 1 ? !ps.decode_as_tiles : ps.spans_as_rows;
-  r.rest_group = r.rest_rows && n == 1 && ps.decode_as_group;
+  r.rest_rows = n == 1 ? !ps.decode_as_tiles : ps.spans_as_rows || n <= ps.short_span;
+  r.rest_group = ps.q8 || (r.rest_rows && n == 1 && ps.decode_as_group);
   // A decode row stays with the vector kernel: alone in its sequence it would fill one of a unit's 64 rows.
   r.few_unit = r.n_few > 0 && n > 1 && ps.few_as_units;
   return r;
@@ -298,6 +304,24 @@ double serial_us(const LaunchRates& rate, double tiles, const RowLoad& r, bool f
   return (few_units ? 17.5 : 24.5) + tiles + std::max(r.bytes / 6.2e6, r.longest / rate.row_alone);
 }
 
+// Workgroups of a row item of an 8-bit pool: K/V heads, times the parts of at most 16 heads of a larger group.
+int q8_row_units(const ic_pool_cfg& c) { return c.num_kv_heads * ((c.num_heads / c.num_kv_heads + 15) / 16); }
+
+// Keys per row item of an 8-bit pool.
+int q8_row_part(const ic_pool* pool, const ic_batch_desc* d, const PlanSizes& ps) {
+  const int64_t units = q8_row_units(pool->cfg), slots = 2 * kExpectedCus;
+  int64_t items = 0, keys = 0;
+  for (int s = 0; s < d->num_seqs && items * units < 2 * slots; ++s) {
+    const SeqRoute rt = route(ps, d->ctx_len[s], d->q_len[s]);
+    if (!rt.rest_rows) continue;
+    const int runs = (d->q_len[s] + ps.item_rows - 1) / ps.item_rows;
+    items += runs;
+    keys += (int64_t)runs * d->ctx_len[s];
+  }
+  if (items == 0 || items * units >= 2 * slots) return kDefaultRowPart;
+  return (int)std::min<int64_t>(kDefaultRowPart, std::max<int64_t>(128, round64((int)(keys * units / (2 * slots)))));
+}
+
 // Keys per decode work item when the caller leaves the choice to the library.  Whole rows (up to kDefaultRowPart keys)
 // as long as they give every workgroup two items; fewer, and part of the chip may idle while the longest rows run: then
 // the partition that is expected to end soonest.  The model, in us:
@@ -314,6 +338,7 @@ double serial_us(const LaunchRates& rate, double tiles, const RowLoad& r, bool f
 // 32 heads of 64 dims, 8 of 1000..3000 31 (768) / 40.  From two rounds on whole rows win: 13B shape, 20 rows of 500..3000
 // 115, in partitions of 1024 keys 123.
 int choose_row_part(const ic_pool* pool, const ic_batch_desc* d, const PlanSizes& ps) {
+  if (ps.q8) return q8_row_part(pool, d, ps);
   const bool group = ps.decode_as_group;
   const int D = pool->cfg.head_dim;
   const int64_t units = group ? pool->cfg.num_kv_heads : pool->cfg.num_heads;
@@ -465,14 +490,14 @@ int choose_span_part(const ic_pool* pool, const ic_batch_desc* d, const PlanSize
   static const int parts[] = {kWholeSpan, 8192, 6144, 4096, 3072, 2560, 2048, 1536, 1280, 1024, 768, 640, 512, 384, 256};
   int best = kWholeSpan, longest = 0;
   for (int s = 0; s < d->num_seqs; ++s)
-    if (d->q_len[s] > 1) longest = std::max(longest, d->ctx_len[s]);
+    if (d->q_len[s] > 1 && d->q_len[s] > ps.short_span) longest = std::max(longest, d->ctx_len[s]);
   double best_us = 0.0;
   for (const int part : parts) {
     if (part >= longest && part != kWholeSpan) continue;  // no other plan than whole tiles
     int64_t items = 0, steps = 0, full = 0, most = 0, split_rows = 0;
     for (int s = 0; s < d->num_seqs; ++s) {
       const int c = d->ctx_len[s], n = d->q_len[s];
-      if (n == 1) continue;
+      if (n == 1 || n <= ps.short_span) continue;
       for (int r0 = route(ps, c, n).n_few; r0 < n; r0 += ps.tile_rows) {
         const int nr = std::min(ps.tile_rows, n - r0), klen = c - n + r0 + nr;
         const int64_t np = (klen - 1) / part + 1;
@@ -508,6 +533,7 @@ int choose_span_part(const ic_pool* pool, const ic_batch_desc* d, const PlanSize
 int split_units(const ic_pool* pool, const PlanSizes& ps) {
   const ic_tuning& t = pool->tune;
   if (t.decode_part_tokens > 0 || t.row_launch > 1 || t.row_slots > 0 || ps.row_part >= kDefaultRowPart || ps.side_by_side) return 0;
+  if (ps.q8) return q8_row_units(pool->cfg);
   return ps.decode_as_group ? pool->cfg.num_kv_heads : pool->cfg.num_heads;
 }
 
@@ -534,10 +560,14 @@ void plan_sizes(const ic_pool* pool, const ic_batch_desc* d, PlanSizes& ps, Room
   ps.spans_as_rows = (t.span_kernel == 1);  // default: MFMA tiles
   ps.decode_as_tiles = ps.tile_g_shift > 0 && t.span_kernel == 2;
   ps.decode_as_group = ps.tile_g_shift > 0 && t.span_kernel == 0;
+  // The row kernel of an 8-bit pool has 16 columns, which rows of a span share; spans of up to two such items need no tile.
+  ps.q8 = is_q8(pool->cfg);
+  ps.item_rows = ps.q8 ? std::max(1, 16 / G) : 1;
+  ps.short_span = ps.q8 && t.span_kernel != 2 ? 2 * ps.item_rows : 0;
   ps.row_part = std::min(t.decode_part_tokens > 0 ? round64(t.decode_part_tokens) : kDefaultRowPart, kMaxRowPart);
   int64_t tiles = 0, few = 0;  // unsplit query tiles; rows of spans with few keys
   for (int s = 0; s < d->num_seqs; ++s)
-    if (d->q_len[s] > 1) {
+    if (d->q_len[s] > 1 && d->q_len[s] > ps.short_span) {
       const int n_few = route(ps, d->ctx_len[s], d->q_len[s]).n_few;
       tiles += (d->q_len[s] - n_few + kTileRows - 1) / kTileRows;
       few += n_few;
@@ -545,12 +575,12 @@ void plan_sizes(const ic_pool* pool, const ic_batch_desc* d, PlanSizes& ps, Room
   // Without tile items the few-key units would be a launch of their own (4-5 us); up to two rounds of one-row items on
   // the vector kernel take no longer.  Measured: 4 chunks of 2 rows from position 0 + 1 decode row, 16 heads, two
   // layers: 30 us as row items, 36 as units.
-  ps.few_as_units = room != kLeast && !ps.spans_as_rows && (tiles > 0 || few * pool->cfg.num_heads > 2 * kExpectedCus);
+  ps.few_as_units = !ps.q8 && room != kLeast && !ps.spans_as_rows && (tiles > 0 || few * pool->cfg.num_heads > 2 * kExpectedCus);
   if (t.span_part_tokens == 0) {
     const int64_t head_groups = pool->cfg.num_heads >> ps.tile_g_shift;
     double row_us = 0.0;
     for (int s = 0; s < d->num_seqs; ++s)
-      if (d->q_len[s] == 1) row_us += d->ctx_len[s] * (4.0 * pool->cfg.head_dim * pool->cfg.num_kv_heads / 5.5e6);
+      if (d->q_len[s] == 1) row_us += d->ctx_len[s] * ((ps.q8 ? 2.0 : 4.0) * pool->cfg.head_dim * pool->cfg.num_kv_heads / 5.5e6);
     ps.span_part = room != kFull || ps.spans_as_rows || tiles * head_groups >= kUnsplitWorkgroups ? kWholeSpan : choose_span_part(pool, d, ps, row_us);
   }
   // Side by side: tile items or few-key units beside rows of a kernel that has a slim build, unless one after the other is
@@ -562,7 +592,7 @@ void plan_sizes(const ic_pool* pool, const ic_batch_desc* d, PlanSizes& ps, Room
     const bool choose = t.decode_part_tokens == 0 && room == kFull, few_units = ps.few_as_units && few > 0;
     const int part_alone = choose ? choose_row_part(pool, d, ps) : ps.row_part;
     double tiles_alone = 0.0;
-    const double tiles_time = t.serial_spans ? 0.0 : tile_load_us(pool, d, ps, &tiles_alone);
+    const double tiles_time = t.serial_spans || ps.q8 ? 0.0 : tile_load_us(pool, d, ps, &tiles_alone);
     if (tiles_time > 0.0 || (few_units && !t.serial_spans)) {
       RowLoad rows = row_load(pool, d, ps, ps.row_part);
       ps.side_by_side = rows.items > 0 && (ps.decode_as_group ? rows.group && ps.slim_group : true);
@@ -600,13 +630,16 @@ void plan_sizes(const ic_pool* pool, const ic_batch_desc* d, PlanSizes& ps, Room
       ps.few_runs += 1;
       ps.few_rows += rt.n_few;
     }
-    for (int i = 0; i < n_as_rows; ++i) {
-      const int klen = c - n + i + 1;
+    for (int i = 0; i < n_as_rows; i += ps.item_rows) {
+      const int nr = std::min(ps.item_rows, n_as_rows - i);
+      const int klen = c - n + i + nr;
       const int parts = (klen + ps.row_part - 1) / ps.row_part;
+      const bool vec = !ps.q8 && (i < rt.n_few || !rt.rest_group);
       in.row_items += parts;
-      if (!rt.few_unit && (i < rt.n_few || !rt.rest_group)) vec_keys += klen;
-      if (i < rt.n_few || !rt.rest_group) ps.vec_items += parts;
-      if (parts > 1) { in.partial_slots += parts; in.merge_rows += 1; ps.row_slots += parts; ps.row_merges += 1; }
+      if (!rt.few_unit && vec) vec_keys += klen;
+      if (vec) ps.vec_items += parts;
+      if (parts > 1 && ps.q8 && n > 1) { in.partial_slots += parts * nr; in.merge_rows += nr; }
+      else if (parts > 1) { in.partial_slots += parts; in.merge_rows += 1; ps.row_slots += parts; ps.row_merges += 1; }
     }
     if (!rt.rest_rows) {
       const int part = n == 1 ? ps.row_part : ps.span_part;
@@ -670,6 +703,12 @@ PlanLaunches plan_launches(const ic_pool* pool, const PlanSizes& ps) {
   const bool rows = ps.vec_items > ps.few_rows, groups = ps.info.row_items > ps.vec_items;
   PlanLaunches how;
   how.side_by_side = ps.side_by_side;
+  if (ps.q8) {
+    how.tile = tiles ? IC_LAUNCH_PER_ITEM : IC_LAUNCH_NONE;
+    how.group = groups ? IC_LAUNCH_PER_ITEM : IC_LAUNCH_NONE;
+    how.row = IC_LAUNCH_NONE;
+    return how;
+  }
   // head_dim <= 128: the persistent tile launch also when no other kernel runs beside it.  Its per-XCD queues keep the
   // query tiles of one (sequence, head) on one L2: 16 chunks of 2048 rows on 16384 keys, 32 heads of 128, then fetch 2.2 x instead
   // of 6.5 x their keys from HBM and take 8.49 instead of 9.06 ms; 8 chunks of 512, 40 heads or 64 over 8, the same either way.
@@ -720,12 +759,16 @@ void plan_fill(const ic_batch_desc* d, const PlanSizes& ps, char* img) {
     const SeqRoute rt = route(ps, c, n);
     const int n_as_rows = rt.rest_rows ? n : rt.n_few;
     if (rt.few_unit) fews[nruns++] = FewItem{nfew, rt.n_few};
-    for (int i = 0; i < n_as_rows; ++i) {
-      const int klen = c - n + i + 1;
+    for (int i = 0; i < n_as_rows; i += ps.item_rows) {
+      const int nr = std::min(ps.item_rows, n_as_rows - i);
+      const int klen = c - n + i + nr;
       const int parts = (klen + ps.row_part - 1) / ps.row_part;
       const int qrow = d->q_start[s] + i;
-      const bool vec = i < rt.n_few || !rt.rest_group;
-      if (parts > 1) {
+      const bool vec = !ps.q8 && (i < rt.n_few || !rt.rest_group);
+      const bool span_parts = parts > 1 && ps.q8 && n > 1;  // partial slots of a tile's kind: merged by the merge kernel
+      if (span_parts) {
+        for (int r = 0; r < nr; ++r) merges[nmerge++] = MergeItem{qrow + r, slot + r * parts, parts, 0};
+      } else if (parts > 1) {
         if (ps.off_arrived > ps.off_slot_merge)
           for (int k = 0; k < parts; ++k) slot_merge[rslot + k] = nrmerge;
         merges[nrmerge++] = MergeItem{qrow, rslot, parts, 0};
@@ -736,9 +779,12 @@ void plan_fill(const ic_batch_desc* d, const PlanSizes& ps, char* img) {
         it.qrow = qrow;
         it.k_begin = k * ps.row_part;
         it.k_end = std::min(klen, (k + 1) * ps.row_part);
-        it.slot = parts > 1 ? rslot++ : -1;
-        it.pad[0] = it.pad[1] = it.pad[2] = 0;
+        it.slot = span_parts ? slot + k : parts > 1 ? rslot++ : -1;
+        it.pad[0] = ps.q8 ? nr : 0;
+        it.pad[1] = ps.q8 ? c - n + i : 0;
+        it.pad[2] = ps.q8 && n > 1 ? parts : 0;
       }
+      if (span_parts) slot += parts * nr;
     }
     if (!rt.rest_rows && rt.n_few < n) {
       // slots first (per tile: rows x partitions), then items ordered partition-major so that the
@@ -1089,6 +1135,8 @@ static int launch_attention(ic_pool* pool, const PlanSizes& ps, float scale, con
   }
   AttnParams p;
   p.pool = (const uint16_t*)pool->base;
+  p.block_bytes = pool->block_bytes;
+  p.row_units = ps.q8 ? q8_row_units(pool->cfg) : 0;
   p.q = (const uint16_t*)dev_q;
   p.out = (uint16_t*)dev_out;
   p.bt_off = (const int32_t*)(ws + ps.off_bt_off);
@@ -1172,6 +1220,15 @@ static int launch_attention(ic_pool* pool, const PlanSizes& ps, float scale, con
       return IC_EHIP;
     }
     if (!ok) return IC_EHIP;
+  } else if (ps.q8) {
+    if (how.tile != IC_LAUNCH_NONE) {
+      ProfScope ps_(pool, IC_K_TILE, st);
+      if (launch_q8_tile(p, D, pool->cfg.dtype, st) != hipSuccess) return IC_EHIP;
+    }
+    if (how.group != IC_LAUNCH_NONE) {
+      ProfScope ps_(pool, IC_K_GROUP, st);
+      if (launch_q8_rows(p, D, pool->cfg.dtype, st) != hipSuccess) return IC_EHIP;
+    }
   } else {
     if (how.tile != IC_LAUNCH_NONE) {
       ProfScope ps_(pool, IC_K_TILE, st);
@@ -1241,12 +1298,35 @@ int paged_attn_plan_create(ic_pool* pool, const ic_batch_desc* desc, void* dev_w
   });
 }
 
+static bool plan_fits(const ic_pool* pool, const ic_plan* plan) {
+  const ic_pool_cfg &a = pool->cfg, &b = plan->cfg;
+  return a.num_blocks == b.num_blocks && a.block_size == b.block_size && a.num_heads == b.num_heads &&
+         a.num_kv_heads == b.num_kv_heads && a.head_dim == b.head_dim && a.dtype == b.dtype && a.layout == b.layout;
+}
+
+// Rows of k_new / v_new into the pool's slots dev_rows, and back.
+static hipError_t write_rows(const ic_pool* pool, const void* k, const void* v, const int32_t* dev_rows, int32_t n, hipStream_t st) {
+  const ic_pool_cfg& c = pool->cfg;
+  if (is_q8(c)) return launch_q8_write(pool->base, pool->block_bytes, c.dtype, k, v, dev_rows, n, c.num_kv_heads, c.head_dim, st);
+  return launch_append(pool->base, k, v, dev_rows, n, c.num_kv_heads, c.head_dim, st);
+}
+static hipError_t read_rows(const ic_pool* pool, void* k, void* v, const int32_t* dev_rows, int32_t n, hipStream_t st) {
+  const ic_pool_cfg& c = pool->cfg;
+  return launch_read(pool->base, pool->block_bytes, c.dtype, k, v, dev_rows, n, c.num_kv_heads, c.head_dim, st);
+}
+
+static int check_read_rows(const ic_pool* pool, int32_t rows, const void* k, const void* v) {
+  if (misaligned(k) || misaligned(v)) return IC_EALIGN;
+  const size_t bytes = (size_t)rows * pool->cfg.num_kv_heads * pool->cfg.head_dim * 2;
+  const auto meet = [](const char* a, size_t na, const char* b, size_t nb) { return a < b + nb && b < a + na; };
+  const char *kc = (const char*)k, *vc = (const char*)v;
+  if (meet(kc, bytes, vc, bytes) || meet(kc, bytes, pool->base, pool->bytes) || meet(vc, bytes, pool->base, pool->bytes)) return IC_EINVAL;
+  return IC_OK;
+}
+
 int paged_attn_planned(ic_pool* pool, const ic_plan* plan, const void* dev_q, void* dev_out, void* hip_stream) {
   if (!pool || !plan || !dev_q || !dev_out) return IC_ENULL;
-  const ic_pool_cfg &a = pool->cfg, &b = plan->cfg;
-  if (a.num_blocks != b.num_blocks || a.block_size != b.block_size || a.num_heads != b.num_heads ||
-      a.num_kv_heads != b.num_kv_heads || a.head_dim != b.head_dim || a.dtype != b.dtype || a.layout != b.layout)
-    return IC_EINVAL;  // the plan was made for another shape
+  if (!plan_fits(pool, plan)) return IC_EINVAL;  // the plan was made for another shape
   if (std::memcmp(&pool->tune, &plan->tune, sizeof(ic_tuning)) != 0) return IC_EINVAL;  // or another launch plan
   if (misaligned(dev_q) || misaligned(dev_out)) return IC_EALIGN;
   return launch_attention(pool, plan->ps, plan->scale, dev_q, dev_out, plan->ws, (hipStream_t)hip_stream);
@@ -1255,17 +1335,24 @@ int paged_attn_planned(ic_pool* pool, const ic_plan* plan, const void* dev_q, vo
 int kv_write_span_planned(ic_pool* pool, const ic_plan* plan, const void* dev_k_new, const void* dev_v_new,
                           void* hip_stream) {
   if (!pool || !plan || !dev_k_new || !dev_v_new) return IC_ENULL;
-  const ic_pool_cfg &a = pool->cfg, &b = plan->cfg;
-  if (a.num_blocks != b.num_blocks || a.block_size != b.block_size || a.num_heads != b.num_heads ||
-      a.num_kv_heads != b.num_kv_heads || a.head_dim != b.head_dim || a.dtype != b.dtype || a.layout != b.layout)
-    return IC_EINVAL;
+  if (!plan_fits(pool, plan)) return IC_EINVAL;
   if (!plan->append_checked) return IC_EDUP;
   if (misaligned(dev_k_new) || misaligned(dev_v_new)) return IC_EALIGN;
   hipStream_t st = (hipStream_t)hip_stream;
   ProfScope ps_(pool, IC_K_APPEND, st);
-  const hipError_t e = launch_append(pool->base, dev_k_new, dev_v_new, (const int32_t*)(plan->ws + plan->ps.off_row_dst),
-                                     plan->total_q_rows, a.num_kv_heads, a.head_dim, st);
-  return e == hipSuccess ? IC_OK : IC_EHIP;
+  return write_rows(pool, dev_k_new, dev_v_new, (const int32_t*)(plan->ws + plan->ps.off_row_dst), plan->total_q_rows, st) == hipSuccess ? IC_OK
+                                                                                                                                       : IC_EHIP;
+}
+
+int kv_read_span_planned(ic_pool* pool, const ic_plan* plan, void* dev_k_out, void* dev_v_out, void* hip_stream) {
+  if (!pool || !plan || !dev_k_out || !dev_v_out) return IC_ENULL;
+  if (!plan_fits(pool, plan)) return IC_EINVAL;
+  const int rc = check_read_rows(pool, plan->total_q_rows, dev_k_out, dev_v_out);
+  if (rc != IC_OK) return rc;
+  hipStream_t st = (hipStream_t)hip_stream;
+  ProfScope ps_(pool, IC_K_READ, st);
+  return read_rows(pool, dev_k_out, dev_v_out, (const int32_t*)(plan->ws + plan->ps.off_row_dst), plan->total_q_rows, st) == hipSuccess ? IC_OK
+                                                                                                                                     : IC_EHIP;
 }
 
 int paged_attn_plan_destroy(ic_plan* plan) {
@@ -1377,8 +1464,29 @@ int kv_write_span(ic_pool* pool, const ic_batch_desc* desc, const void* dev_k_ne
   hipError_t e;
   {
     ProfScope ps_(pool, IC_K_APPEND, st);
-    e = launch_append(pool->base, dev_k_new, dev_v_new, pool->lists[kListAppend].dev, desc->total_q_rows,
-                      pool->cfg.num_kv_heads, pool->cfg.head_dim, st);
+    e = write_rows(pool, dev_k_new, dev_v_new, pool->lists[kListAppend].dev, desc->total_q_rows, st);
+  }
+  return e == hipSuccess ? IC_OK : IC_EHIP;
+  });
+}
+
+int kv_read_span(ic_pool* pool, const ic_batch_desc* desc, void* dev_k_out, void* dev_v_out, void* hip_stream) {
+  if (!pool || !desc || !dev_k_out || !dev_v_out) return IC_ENULL;
+  return guarded([&]() -> int {
+  int rc = check_batch(pool->cfg, desc, (desc->flags & IC_FLAG_TRUSTED) != 0);
+  if (rc != IC_OK) return rc;
+  if ((rc = check_read_rows(pool, desc->total_q_rows, dev_k_out, dev_v_out)) != IC_OK) return rc;
+  const size_t rows = (size_t)desc->total_q_rows;
+  std::vector<int32_t> src(rows, -1);
+  append_destinations(desc, src.data());
+  hipStream_t st = (hipStream_t)hip_stream;
+  // The append's list: reading back what was just written uploads nothing.  (Not checked for two rows on one slot: a write of the
+  // same rows still checks that.)
+  if ((rc = upload_list(pool, kListAppend, src.data(), rows, false, st)) != IC_OK) return rc;
+  hipError_t e;
+  {
+    ProfScope ps_(pool, IC_K_READ, st);
+    e = read_rows(pool, dev_k_out, dev_v_out, pool->lists[kListAppend].dev, desc->total_q_rows, st);
   }
   return e == hipSuccess ? IC_OK : IC_EHIP;
   });

@@ -28,6 +28,8 @@ constexpr int tile_rows(int head_dim) { return head_dim <= 128 ? 256 : 128; }
 
 // One work item of the row kernel: one query row against keys [k_begin, k_end) of its sequence,
 // for every head (the head is a grid dimension).  32 bytes so a wave reads it with scalar loads.
+// 8-bit pools: pad = {n_rows, pos0, nparts}: n_rows consecutive rows from qrow, the first at position pos0, each against the keys up to
+// its own position; partial slot of row r: slot + r * nparts.  nparts 0: a decode row, which its last partition may merge.
 struct RowItem {
   int32_t seq;      // index into bt_off
   int32_t qrow;     // row in packed q / out
@@ -67,7 +69,8 @@ struct MergeItem {
 };
 
 struct AttnParams {
-  const uint16_t* pool;
+  const uint16_t* pool;    // bf16 pools: the cache; 8-bit pools: base of the blocks
+  uint64_t block_bytes;
   const uint16_t* q;
   uint16_t* out;
   const int32_t* bt_off;   // [num_seqs] offset of each sequence's ids in bt_flat
@@ -93,6 +96,7 @@ struct AttnParams {
   int32_t merge_first;     // merge items [merge_first, merge_first + n_merge_items) are the merge kernel's
   int32_t n_merge_items;
   int32_t split_units;     // units of a split decode row merged by its last partition (heads, or K/V heads on the group kernel); 0: none is
+  int32_t row_units;       // 8-bit pools: workgroups per row item (K/V heads x 16-head parts of a group)
   float scale_log2e;       // scale * log2(e): scores are kept in log2 units
   int32_t row_variant;     // row-kernel build: bit0 = prefetch depth 2, bit1 = plain (cached) loads
   int32_t tile_first;      // persistent tile kernel: its waves ask for issue priority over the kernel beside it
@@ -158,6 +162,14 @@ hipError_t launch_group_slim(const AttnParams& p, int head_dim, int slots, hipSt
 // Rows of k_new / v_new ([rows][H][D] bf16) into the pool at slot dst[row] (block * 16 + slot; < 0: skip).
 hipError_t launch_append(void* pool, const void* k_new, const void* v_new, const int32_t* dev_dst, int32_t rows,
                          int num_heads, int head_dim, hipStream_t st);
+// The 8-bit pools' kernels; dtype: IC_DTYPE_E4M3 or IC_DTYPE_INT8.
+hipError_t launch_q8_rows(const AttnParams& p, int head_dim, int dtype, hipStream_t st);  // row items x row_units
+hipError_t launch_q8_tile(const AttnParams& p, int head_dim, int dtype, hipStream_t st);
+hipError_t launch_q8_write(void* pool, size_t block_bytes, int dtype, const void* k_new, const void* v_new, const int32_t* dev_dst, int32_t rows,
+                           int num_heads, int head_dim, hipStream_t st);
+// Slots dev_src[row] of a pool of any dtype into rows of k_out / v_out.
+hipError_t launch_read(const void* pool, size_t block_bytes, int dtype, void* k_out, void* v_out, const int32_t* dev_src, int32_t rows,
+                       int num_heads, int head_dim, hipStream_t st);
 // bytes: multiple of 16; pinned_src: pinned host memory (device-visible); dev_dst: device, 16-byte aligned.
 hipError_t launch_upload(void* dev_dst, const void* pinned_src, size_t bytes, hipStream_t st);
 hipError_t launch_pack(const void* pool, void* staging, const int32_t* dev_ids, int32_t n,
