@@ -26,7 +26,7 @@ struct Impl<tile16::kDim> {
   static constexpr int kThreads = tile16::kThreads;
   static constexpr int kLdsBytes = std::max(tile16::kLdsBytes, fewp::few_lds_bytes<tile16::kDim>());
   static __device__ __forceinline__ void body(const AttnParams& p, const TileItem& it, int th, uint16_t* lds) {
-    tile16::tile16_body(p, it, th, lds);
+    tile16::tile16_body<>(p, it, th, lds);
   }
 };
 

@@ -704,7 +704,7 @@ PlanLaunches plan_launches(const ic_pool* pool, const PlanSizes& ps) {
   PlanLaunches how;
   how.side_by_side = ps.side_by_side;
   if (ps.q8) {
-    how.tile = tiles ? IC_LAUNCH_PER_ITEM : IC_LAUNCH_NONE;
+    how.tile = tiles ? IC_LAUNCH_PERSISTENT : IC_LAUNCH_NONE;
     how.group = groups ? IC_LAUNCH_PER_ITEM : IC_LAUNCH_NONE;
     how.row = IC_LAUNCH_NONE;
     return how;
@@ -1223,7 +1223,7 @@ static int launch_attention(ic_pool* pool, const PlanSizes& ps, float scale, con
   } else if (ps.q8) {
     if (how.tile != IC_LAUNCH_NONE) {
       ProfScope ps_(pool, IC_K_TILE, st);
-      if (launch_q8_tile(p, D, pool->cfg.dtype, st) != hipSuccess) return IC_EHIP;
+      if (launch_q8_tile(p, D, pool->cfg.dtype, pool->num_cus, st) != hipSuccess) return IC_EHIP;
     }
     if (how.group != IC_LAUNCH_NONE) {
       ProfScope ps_(pool, IC_K_GROUP, st);

@@ -164,7 +164,7 @@ hipError_t launch_append(void* pool, const void* k_new, const void* v_new, const
                          int num_heads, int head_dim, hipStream_t st);
 // The 8-bit pools' kernels; dtype: IC_DTYPE_E4M3 or IC_DTYPE_INT8.
 hipError_t launch_q8_rows(const AttnParams& p, int head_dim, int dtype, hipStream_t st);  // row items x row_units
-hipError_t launch_q8_tile(const AttnParams& p, int head_dim, int dtype, hipStream_t st);
+hipError_t launch_q8_tile(const AttnParams& p, int head_dim, int dtype, int slots, hipStream_t st);
 hipError_t launch_q8_write(void* pool, size_t block_bytes, int dtype, const void* k_new, const void* v_new, const int32_t* dev_dst, int32_t rows,
                            int num_heads, int head_dim, hipStream_t st);
 // Slots dev_src[row] of a pool of any dtype into rows of k_out / v_out.

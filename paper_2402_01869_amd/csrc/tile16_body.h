@@ -124,7 +124,10 @@ __device__ __forceinline__ void weight_op(f32x4 (&s)[2], bf16x8& pw, float negm,
 
 // One TileItem x one group of (1 << p.tile_g_shift) query heads that share a K/V head, executed by a workgroup of kWaves
 // waves (see tile32_body() for the row mapping and for the steps, which are the same).  lds: kLdsBytes, 1 KiB aligned.
+// FMT: what the pool holds, as in tile32_body().
+template <int FMT = IC_DTYPE_BF16>
 __device__ __forceinline__ void tile16_body(const AttnParams& p, const TileItem& it, int th, uint16_t* lds) {
+  constexpr bool kQ8 = FMT != IC_DTYPE_BF16;
   const int32_t offs = first_offsets(p);
   constexpr int D = kDim, kS = kQ + kP, kR = kRegions;
   typedef __attribute__((address_space(3))) const char lds_char;
@@ -177,9 +180,36 @@ __device__ __forceinline__ void tile16_body(const AttnParams& p, const TileItem&
   int id_u = block_id(0), id_1 = block_id(1), id_2 = block_id(2);  // blocks of tiles u, u + 1, u + 2
 #pragma unroll
   for (int s = 0; s < D / 32; ++s) asm volatile("" ::"v"(q[s]));  // waits
-  copy_tile(id_u, 0, 0);
-  if (n_tiles > 1) copy_tile(id_1, 0, kTileBytes);
-  copy_tile(id_u, vplane, kVBuf);
+  q8::Stager<D, kQ8 ? FMT : IC_DTYPE_E4M3> stager(p, kvh, Hk, lane, my_key, spread(my_key));
+  q8::Codes<D> kcode, vcode;
+  int id_3 = 0;  // block of tile u + 3 (8-bit pools: the codes of a tile are loaded a step before it is stored)
+  auto store_tile = [&](auto kv_tag, const q8::Codes<D>& codes, int buf) __attribute__((always_inline)) {
+    const float f = stager.template factor<decltype(kv_tag)::value>(codes);
+    unroll<stager.kPieces>([&](auto k) __attribute__((always_inline)) { stager.template store<decltype(k)::value>(codes, f, my_lds + (uint32_t)buf); });
+  };
+  constexpr std::integral_constant<int, 0> kK{};
+  constexpr std::integral_constant<int, 1> kV{};
+  if constexpr (kQ8) {
+    q8::Codes<D> k1;
+    stager.template load<0>(kcode, id_u);
+    if (n_tiles > 1) stager.template load<0>(k1, id_1);
+    stager.template load<1>(vcode, id_u);
+    id_3 = block_id(3);
+    store_tile(kK, kcode, 0);
+    if (n_tiles > 1) store_tile(kK, k1, kTileBytes);
+    store_tile(kV, vcode, kVBuf);
+    if (n_tiles > 2) stager.template load<0>(kcode, id_2);
+    if (n_tiles > 1) stager.template load<1>(vcode, id_1);
+  } else {
+    copy_tile(id_u, 0, 0);
+    if (n_tiles > 1) copy_tile(id_1, 0, kTileBytes);
+    copy_tile(id_u, vplane, kVBuf);
+  }
+  // Barriers of a step: what was copied, or stored, a step ago is there.
+  auto meet = [&]() __attribute__((always_inline)) {
+    if constexpr (kQ8) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else barrier<kR>();
+  };
 
   // ---- Q^T, O^T = 0, normaliser = 0
   {
@@ -258,7 +288,12 @@ __device__ __forceinline__ void tile16_body(const AttnParams& p, const TileItem&
   auto next_ids = [&](int u) __attribute__((always_inline)) {
     id_u = id_1;
     id_1 = id_2;
-    id_2 = block_id(u + 3);
+    if constexpr (kQ8) {
+      id_2 = id_3;
+      id_3 = block_id(u + 4);
+    } else {
+      id_2 = block_id(u + 3);
+    }
   };
   auto hide = [&](f32x4 (&s)[2], int k0) __attribute__((always_inline)) {  // scores of keys past the lane's row; returns the largest left
     const int ln = here();
@@ -295,9 +330,9 @@ __device__ __forceinline__ void tile16_body(const AttnParams& p, const TileItem&
     const int par = (u & 1) * kTileBytes, other = par ^ kTileBytes;
     const int kt = it.k_begin + u * kTileK;
     const int n_valid = it.k_end - (kt - kTileK);
-    if (u >= n_tiles - 1 && u > 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no copy follows V of tile u - 1
+    if (!kQ8 && u >= n_tiles - 1 && u > 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no copy follows V of tile u - 1
     if (n_valid < kTileK) {  // dead slots of that tile: zero (0 * NaN would poison the product)
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if constexpr (!kQ8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       const int at = here();
       if (8 * w + (at >> 3) >= n_valid) {
 #pragma unroll
@@ -305,10 +340,15 @@ __device__ __forceinline__ void tile16_body(const AttnParams& p, const TileItem&
           *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(my_lds + (uint32_t)(kVBuf + other + 1024 * j) + 16 * at) = (u32x4){0u, 0u, 0u, 0u};
       }
     }
-    if (u == 0 && n_tiles > 1) barrier<2 * kR>();  // K of the second tile and V of the first may be on their way
-    else barrier<kR>();
+    if (!kQ8 && u == 0 && n_tiles > 1) barrier<2 * kR>();  // K of the second tile and V of the first may be on their way
+    else meet();
     const int vt = n_tiles == 2 ? u + 1 : u;  // (no third tile needs the wait for V of the second to be by count)
-    if (vt > 0 && vt < n_tiles) copy_tile(vt == u ? id_u : id_1, vplane, __builtin_amdgcn_readfirstlane(kVBuf + (vt & 1) * kTileBytes));
+    if constexpr (kQ8) {
+      if (u > 0 && u < n_tiles) {
+        store_tile(kV, vcode, __builtin_amdgcn_readfirstlane(kVBuf + par));
+        stager.template load<1>(vcode, id_1);
+      }
+    } else if (vt > 0 && vt < n_tiles) copy_tile(vt == u ? id_u : id_1, vplane, __builtin_amdgcn_readfirstlane(kVBuf + (vt & 1) * kTileBytes));
     if (u > 0 && 2 * u - 2 < n_half) {
       products(std::integral_constant<int, 0>{}, pa, other);
       normaliser<false>(pa);
@@ -361,11 +401,18 @@ __device__ __forceinline__ void tile16_body(const AttnParams& p, const TileItem&
     // No tile to publish, and no copy into the buffer that this one leaves.  (From three tiles on the last step is some waves' fast one,
     // which has the barrier; the waves of a workgroup must meet at the same ones.)
     if (n_tiles <= 2 && u + 1 == n_tiles) return;
-    barrier<kR>();
-    if (u + 2 < n_tiles) copy_tile(id_2, 0, par);
-    next_ids(u);
+    meet();
+    if constexpr (kQ8) {
+      if (u + 2 < n_tiles) store_tile(kK, kcode, __builtin_amdgcn_readfirstlane(par));
+      next_ids(u);
+      if (u + 3 < n_tiles) stager.template load<0>(kcode, id_2);
+    } else {
+      if (u + 2 < n_tiles) copy_tile(id_2, 0, par);
+      next_ids(u);
+    }
   };
 
+  [[maybe_unused]] float factor;  // of the codes that a stage stores
   // Operands are read four MFMAs ahead (an MFMA is half as long as the 32-row shape's).
   auto fast_stage = [&](auto half_tag, auto par_tag, int u, f32x4 (&scur)[2], f32x4 (&snext)[2], bf16x8& pcur, bf16x8& pprev) __attribute__((always_inline)) {
     constexpr int kHalf = decltype(half_tag)::value, kPar = decltype(par_tag)::value;
@@ -385,7 +432,7 @@ __device__ __forceinline__ void tile16_body(const AttnParams& p, const TileItem&
     unroll<kQ>([&](auto ii) __attribute__((always_inline)) {
       constexpr int i = decltype(ii)::value;
       if constexpr (i == kQ - 4) {
-        barrier<kR>();
+        meet();
         pin();
       }
       if constexpr (i % 2 == 0) asm volatile("" ::"v"(kop[i]), "v"(kop[i + 1]));  // one wait for the two
@@ -408,10 +455,24 @@ __device__ __forceinline__ void tile16_body(const AttnParams& p, const TileItem&
         operand_v(std::integral_constant<int, i + 4>{});
         operand_v(std::integral_constant<int, i + 5>{});
       }
-      if constexpr (i == 0 && kHalf == 0) copy_tile(id_u, vplane, kVBuf + kPar * kTileBytes);
-      if constexpr (i == 0 && kHalf == 1) {
-        copy_tile(id_2, 0, kPar * kTileBytes);
-        next_ids(u);
+      if constexpr (kQ8) {  // a piece a slot
+        const q8::Codes<D>& codes = kHalf == 0 ? vcode : kcode;
+        if constexpr (i == 0) factor = stager.template factor<kHalf ^ 1>(codes);
+        if constexpr (i < stager.kPieces) stager.template store<i>(codes, factor, my_lds + (uint32_t)((kHalf ? 0 : kVBuf) + kPar * kTileBytes));
+        if constexpr (i == stager.kPieces) {
+          if constexpr (kHalf == 0) {
+            stager.template load<1>(vcode, id_1);
+          } else {
+            next_ids(u);
+            stager.template load<0>(kcode, id_2);
+          }
+        }
+      } else {
+        if constexpr (i == 0 && kHalf == 0) copy_tile(id_u, vplane, kVBuf + kPar * kTileBytes);
+        if constexpr (i == 0 && kHalf == 1) {
+          copy_tile(id_2, 0, kPar * kTileBytes);
+          next_ids(u);
+        }
       }
       if constexpr (i >= kP - 4) kop[i - (kP - 4)] = read_k(i - (kP - 4), kNextAt);
       weights(std::integral_constant<int, kQ + i>{});

@@ -39,6 +39,7 @@
 #include <type_traits>
 #include <utility>
 
+#include "q8_stage.h"
 #include "tile_body.h"
 
 namespace ic {
@@ -210,9 +211,12 @@ __device__ __forceinline__ void weight_op(f32x16& s, bf16x8 (&pw)[2], float negm
 // head (th << shift) + (r & mask): with multi-head attention (shift 0) a tile is 256 rows of one head,
 // with grouped-query attention the heads of a group ride on one staging of their common keys.
 // lds: at least tile32_lds_bytes<D>() bytes of workgroup LDS, 1 KiB aligned.
-template <int D>
+// FMT: what the pool holds (IC_DTYPE_*).  An 8-bit pool's tiles pass through registers, where their codes become bf16 (q8_stage.h): what is
+// copied below is stored there, at the same two places of a step, from codes that were loaded a step before.
+template <int D, int FMT = IC_DTYPE_BF16>
 __device__ __forceinline__ void tile32_body(const AttnParams& p, const TileItem& it, int th, uint16_t* lds) {
   using G = G32<D>;
+  constexpr bool kQ8 = FMT != IC_DTYPE_BF16;
   constexpr int kQ = G::kQSteps, kP = 2 * G::kDTiles, kS = kQ + kP, kR = G::kRegions;
   const int32_t offs = first_offsets(p);
   typedef __attribute__((address_space(3))) const char lds_char;
@@ -272,9 +276,36 @@ __device__ __forceinline__ void tile32_body(const AttnParams& p, const TileItem&
   int id_u = block_id(0), id_1 = block_id(1), id_2 = block_id(2);  // blocks of tiles u, u + 1, u + 2
 #pragma unroll
   for (int s = 0; s < kQ; ++s) asm volatile("" ::"v"(q[s]));  // waits
-  copy_tile(id_u, 0, 0);
-  if (n_tiles > 1) copy_tile(id_1, 0, G::kTileBytes);
-  copy_tile(id_u, vplane, kVBuf);
+  q8::Stager<D, kQ8 ? FMT : IC_DTYPE_E4M3> stager(p, kvh, Hk, lane, my_key, spread(my_key));
+  q8::Codes<D> kcode, vcode;
+  int id_3 = 0;  // block of tile u + 3 (8-bit pools: the codes of a tile are loaded a step before it is stored)
+  auto store_tile = [&](auto kv_tag, const q8::Codes<D>& codes, int buf) __attribute__((always_inline)) {
+    const float f = stager.template factor<decltype(kv_tag)::value>(codes);
+    unroll<stager.kPieces>([&](auto k) __attribute__((always_inline)) { stager.template store<decltype(k)::value>(codes, f, my_lds + (uint32_t)buf); });
+  };
+  constexpr std::integral_constant<int, 0> kK{};
+  constexpr std::integral_constant<int, 1> kV{};
+  if constexpr (kQ8) {
+    q8::Codes<D> k1;
+    stager.template load<0>(kcode, id_u);
+    if (n_tiles > 1) stager.template load<0>(k1, id_1);
+    stager.template load<1>(vcode, id_u);
+    id_3 = block_id(3);
+    store_tile(kK, kcode, 0);
+    if (n_tiles > 1) store_tile(kK, k1, G::kTileBytes);
+    store_tile(kV, vcode, kVBuf);
+    if (n_tiles > 2) stager.template load<0>(kcode, id_2);
+    if (n_tiles > 1) stager.template load<1>(vcode, id_1);
+  } else {
+    copy_tile(id_u, 0, 0);
+    if (n_tiles > 1) copy_tile(id_1, 0, G::kTileBytes);
+    copy_tile(id_u, vplane, kVBuf);
+  }
+  // Barriers of a step: what was copied, or stored, a step ago is there.
+  auto meet = [&]() __attribute__((always_inline)) {
+    if constexpr (kQ8) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else barrier<kR>();
+  };
 
   // ---- Q^T, O^T = 0, normaliser = 0
   {
@@ -379,7 +410,12 @@ __device__ __forceinline__ void tile32_body(const AttnParams& p, const TileItem&
   auto next_ids = [&](int u) __attribute__((always_inline)) {
     id_u = id_1;
     id_1 = id_2;
-    id_2 = block_id(u + 3);
+    if constexpr (kQ8) {
+      id_2 = id_3;
+      id_3 = block_id(u + 4);
+    } else {
+      id_2 = block_id(u + 3);
+    }
   };
 
   auto hide = [&](f32x16& s, int k0) __attribute__((always_inline)) {  // scores of keys past the lane's row; returns the largest left
@@ -417,9 +453,9 @@ __device__ __forceinline__ void tile32_body(const AttnParams& p, const TileItem&
     const int par = (u & 1) * G::kTileBytes, other = par ^ G::kTileBytes;
     const int kt = it.k_begin + u * kTileK;
     const int n_valid = it.k_end - (kt - kTileK);
-    if (u >= n_tiles - 1 && u > 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no copy follows V of tile u - 1
+    if (!kQ8 && u >= n_tiles - 1 && u > 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no copy follows V of tile u - 1
     if (n_valid < kTileK) {  // dead slots of that tile: zero (0 * NaN would poison the product)
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if constexpr (!kQ8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       const int at = here();
       if (8 * w + (at >> 3) >= n_valid) {
 #pragma unroll
@@ -427,10 +463,15 @@ __device__ __forceinline__ void tile32_body(const AttnParams& p, const TileItem&
           *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(my_lds + (uint32_t)(kVBuf + other + 1024 * j) + 16 * at) = (u32x4){0u, 0u, 0u, 0u};
       }
     }
-    if (u == 0 && n_tiles > 1) barrier<2 * kR>();  // K of the second tile and V of the first may be on their way
-    else barrier<kR>();
+    if (!kQ8 && u == 0 && n_tiles > 1) barrier<2 * kR>();  // K of the second tile and V of the first may be on their way
+    else meet();
     const int vt = n_tiles == 2 ? u + 1 : u;  // (no third tile needs the wait for V of the second to be by count)
-    if (vt > 0 && vt < n_tiles) copy_tile(vt == u ? id_u : id_1, vplane, __builtin_amdgcn_readfirstlane(kVBuf + (vt & 1) * G::kTileBytes));
+    if constexpr (kQ8) {
+      if (u > 0 && u < n_tiles) {
+        store_tile(kV, vcode, __builtin_amdgcn_readfirstlane(kVBuf + par));
+        stager.template load<1>(vcode, id_1);
+      }
+    } else if (vt > 0 && vt < n_tiles) copy_tile(vt == u ? id_u : id_1, vplane, __builtin_amdgcn_readfirstlane(kVBuf + (vt & 1) * G::kTileBytes));
     if (u > 0 && 2 * u - 2 < n_half) {
       products(std::integral_constant<int, 0>{}, pa, other);
       normaliser<D, false>(pa[0]);
@@ -489,11 +530,18 @@ __device__ __forceinline__ void tile32_body(const AttnParams& p, const TileItem&
     // No tile to publish, and no copy into the buffer that this one leaves.  (From three tiles on the last step is some waves' fast one,
     // which has the barrier; the waves of a workgroup must meet at the same ones.)
     if (n_tiles <= 2 && u + 1 == n_tiles) return;
-    barrier<kR>();
-    if (u + 2 < n_tiles) copy_tile(id_2, 0, par);
-    next_ids(u);
+    meet();
+    if constexpr (kQ8) {
+      if (u + 2 < n_tiles) store_tile(kK, kcode, __builtin_amdgcn_readfirstlane(par));
+      next_ids(u);
+      if (u + 3 < n_tiles) stager.template load<0>(kcode, id_2);
+    } else {
+      if (u + 2 < n_tiles) copy_tile(id_2, 0, par);
+      next_ids(u);
+    }
   };
 
+  [[maybe_unused]] float factor;  // of the codes that a stage stores
   auto fast_stage = [&](auto half_tag, auto par_tag, int u, f32x16& scur, f32x16& snext, bf16x8 (&pcur)[2], bf16x8 (&pprev)[2]) __attribute__((always_inline)) {
     constexpr int kHalf = decltype(half_tag)::value, kPar = decltype(par_tag)::value;
     constexpr int kAt = kPar * G::kTileBytes + kHalf * 2 * G::kKeyGroup;
@@ -518,7 +566,7 @@ __device__ __forceinline__ void tile32_body(const AttnParams& p, const TileItem&
     unroll<kQ>([&](auto ii) __attribute__((always_inline)) {
       constexpr int i = decltype(ii)::value;
       if constexpr (i == kQ - 2) {
-        barrier<kR>();
+        meet();
         pin();
       }
       if constexpr (i % 2 == 0) asm volatile("" ::"v"(kop[i]), "v"(kop[i + 1]));  // one wait for the two
@@ -541,10 +589,24 @@ __device__ __forceinline__ void tile32_body(const AttnParams& p, const TileItem&
         operand_v(std::integral_constant<int, i + 2>{});
         operand_v(std::integral_constant<int, i + 3>{});
       }
-      if constexpr (i == 0 && kHalf == 0) copy_tile(id_u, vplane, kVBuf + kPar * G::kTileBytes);
-      if constexpr (i == 0 && kHalf == 1) {
-        copy_tile(id_2, 0, kPar * G::kTileBytes);
-        next_ids(u);
+      if constexpr (kQ8) {  // a piece a slot
+        const q8::Codes<D>& codes = kHalf == 0 ? vcode : kcode;
+        if constexpr (i == 0) factor = stager.template factor<kHalf ^ 1>(codes);
+        if constexpr (i < stager.kPieces) stager.template store<i>(codes, factor, my_lds + (uint32_t)((kHalf ? 0 : kVBuf) + kPar * G::kTileBytes));
+        if constexpr (i == stager.kPieces) {
+          if constexpr (kHalf == 0) {
+            stager.template load<1>(vcode, id_1);
+          } else {
+            next_ids(u);
+            stager.template load<0>(kcode, id_2);
+          }
+        }
+      } else {
+        if constexpr (i == 0 && kHalf == 0) copy_tile(id_u, vplane, kVBuf + kPar * G::kTileBytes);
+        if constexpr (i == 0 && kHalf == 1) {
+          copy_tile(id_2, 0, kPar * G::kTileBytes);
+          next_ids(u);
+        }
       }
       if constexpr (i >= kP - 2) kop[i - (kP - 2)] = read_k(i - (kP - 2), kNextAt);
       weights(std::integral_constant<int, kQ + i>{});
