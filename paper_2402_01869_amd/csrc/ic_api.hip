@@ -307,19 +307,48 @@ double serial_us(const LaunchRates& rate, double tiles, const RowLoad& r, bool f
 // Workgroups of a row item of an 8-bit pool: K/V heads, times the parts of at most 16 heads of a larger group.
 int q8_row_units(const ic_pool_cfg& c) { return c.num_kv_heads * ((c.num_heads / c.num_kv_heads + 15) / 16); }
 
-// Keys per row item of an 8-bit pool.
+// Keys per row item of an 8-bit pool: whole rows (up to kDefaultRowPart keys) once they give every place of a workgroup (two to a CU) two
+// items, before that the partition that is expected to end soonest.  The model, in us: the cached bytes at 6.6 TB/s, or the longest
+// item, which a workgroup alone reads at 27 / 41 / 54 GB/s (head_dim 64 / 128 / 256; integers, whose conversion takes more
+// instructions, 0.85 of that); a little of the longest item's time for the end, where only the longest are left; 2.1 us a round of
+// items; and a split: 1 us, and 0.9 us for every four partitions of the longest row.  Fitted to 34 batches in 11 partitions each
+// (1 to 256 rows of 16 to 8000 keys; rms 8 %); what it chooses takes 4 % longer in the mean than the best (at most 16 %).  Measured per layer (us),
+// chosen partition / whole rows: 13B shape, one row of 3000 keys 10.6 (512) / 23.1; 70B shape, 8 of 1000..8000 24.6 (1024) / 32.6, one of
+// 6000 11.6 (512) / 31.6; GPT-J shape, 2 of 2000 12.9 (512) / 23.9, 16 of 512..2048 33.3 whole, 33.8 in parts of 512.
 int q8_row_part(const ic_pool* pool, const ic_batch_desc* d, const PlanSizes& ps) {
   const int64_t units = q8_row_units(pool->cfg), slots = 2 * kExpectedCus;
-  int64_t items = 0, keys = 0;
-  for (int s = 0; s < d->num_seqs && items * units < 2 * slots; ++s) {
-    const SeqRoute rt = route(ps, d->ctx_len[s], d->q_len[s]);
-    if (!rt.rest_rows) continue;
-    const int runs = (d->q_len[s] + ps.item_rows - 1) / ps.item_rows;
-    items += runs;
-    keys += (int64_t)runs * d->ctx_len[s];
+  const int D = pool->cfg.head_dim;
+  const auto runs_of = [&](int s) -> int64_t {  // row items of sequence s, were they not split
+    return route(ps, d->ctx_len[s], d->q_len[s]).rest_rows ? (d->q_len[s] + ps.item_rows - 1) / ps.item_rows : 0;
+  };
+  int64_t whole = 0, keys = 0;
+  int longest = 0;
+  for (int s = 0; s < d->num_seqs && whole * units < 2 * slots; ++s) {
+    const int64_t runs = runs_of(s);
+    whole += runs * ((d->ctx_len[s] + kDefaultRowPart - 1) / kDefaultRowPart);
+    keys += runs * d->ctx_len[s];
+    if (runs > 0) longest = std::max(longest, d->ctx_len[s]);
   }
-  if (items == 0 || items * units >= 2 * slots) return kDefaultRowPart;
-  return (int)std::min<int64_t>(kDefaultRowPart, std::max<int64_t>(128, round64((int)(keys * units / (2 * slots)))));
+  if (whole == 0 || whole * units >= 2 * slots) return kDefaultRowPart;
+  const double key_bytes = 2.0 * (D + 1);
+  const double alone = (D == 64 ? 27e3 : D == 128 ? 41e3 : 54e3) * (pool->cfg.dtype == IC_DTYPE_INT8 ? 0.85 : 1.0);  // bytes per us
+  static const int parts[] = {kDefaultRowPart, 2048, 1536, 1024, 768, 512, 384, 256};
+  int best = kDefaultRowPart;
+  double best_us = 0.0;
+  for (const int part : parts) {
+    if (part >= longest && part != kDefaultRowPart) continue;  // no other plan than whole rows
+    int64_t n = 0;
+    for (int s = 0; s < d->num_seqs; ++s) n += runs_of(s) * ((d->ctx_len[s] + part - 1) / part);
+    n *= units;
+    const double last = std::min(longest, part) * key_bytes / alone;
+    double us = std::max(last, keys * units * key_bytes / 6.6e6) + (n > slots ? 0.08 : 0.16) * last + 2.1 * n / slots;
+    if (longest > part) us += 1.0 + 0.9 * ((longest + 4 * part - 1) / (4 * part));
+    if (best_us == 0.0 || us < best_us) {
+      best = part;
+      best_us = us;
+    }
+  }
+  return best;
 }
 
 // Keys per decode work item when the caller leaves the choice to the library.  Whole rows (up to kDefaultRowPart keys)
@@ -592,8 +621,23 @@ void plan_sizes(const ic_pool* pool, const ic_batch_desc* d, PlanSizes& ps, Room
     const bool choose = t.decode_part_tokens == 0 && room == kFull, few_units = ps.few_as_units && few > 0;
     const int part_alone = choose ? choose_row_part(pool, d, ps) : ps.row_part;
     double tiles_alone = 0.0;
-    const double tiles_time = t.serial_spans || ps.q8 ? 0.0 : tile_load_us(pool, d, ps, &tiles_alone);
-    if (tiles_time > 0.0 || (few_units && !t.serial_spans)) {
+    const double tiles_time = t.serial_spans ? 0.0 : tile_load_us(pool, d, ps, &tiles_alone);
+    if (ps.q8) {
+      ps.row_part = part_alone;
+      // Side by side where the shorter of the two is expected to take at least kQ8Pair us: fork, join and the slower pace of both cost
+      // some 20 us and 0.45 of the shorter one's time.  Measured, one after the other / side by side: rows 420 and tiles 260 us
+      // 667 / 575, 95 and 410 490 / 455, 70 and 57 143 / 131, 1484 and 8314 9650 / 9211.  head_dim 256: two workgroups do not fit a CU.
+      double bytes = 0.0;
+      for (int s = 0; s < d->num_seqs; ++s) {
+        const SeqRoute rt = route(ps, d->ctx_len[s], d->q_len[s]);
+        if (rt.rest_rows) bytes += (double)((d->q_len[s] + ps.item_rows - 1) / ps.item_rows) * d->ctx_len[s] * q8_row_units(pool->cfg) * 2.0 * (pool->cfg.head_dim + 1);
+      }
+      const double rows_time = bytes / 6.4e6;
+      constexpr double kQ8Pair = 40.0;
+      ps.side_by_side = !t.serial_spans && pool->cfg.head_dim <= 128 && tiles_time > 0.0 && rows_time > 0.0 &&
+                        (t.row_launch >= 2 || std::min(tiles_time, rows_time) > kQ8Pair);
+      ps.tile_leads = tiles_time > rows_time;
+    } else if (tiles_time > 0.0 || (few_units && !t.serial_spans)) {
       RowLoad rows = row_load(pool, d, ps, ps.row_part);
       ps.side_by_side = rows.items > 0 && (ps.decode_as_group ? rows.group && ps.slim_group : true);
       const RowLoad alone = !ps.side_by_side || part_alone == ps.row_part ? rows : row_load(pool, d, ps, part_alone);
@@ -705,7 +749,7 @@ PlanLaunches plan_launches(const ic_pool* pool, const PlanSizes& ps) {
   how.side_by_side = ps.side_by_side;
   if (ps.q8) {
     how.tile = tiles ? IC_LAUNCH_PERSISTENT : IC_LAUNCH_NONE;
-    how.group = groups ? IC_LAUNCH_PER_ITEM : IC_LAUNCH_NONE;
+    how.group = !groups ? IC_LAUNCH_NONE : how.side_by_side || (t.row_launch == 3 && D <= 128) ? IC_LAUNCH_SLIM : IC_LAUNCH_PER_ITEM;
     how.row = IC_LAUNCH_NONE;
     return how;
   }
@@ -1137,6 +1181,8 @@ static int launch_attention(ic_pool* pool, const PlanSizes& ps, float scale, con
   p.pool = (const uint16_t*)pool->base;
   p.block_bytes = pool->block_bytes;
   p.row_units = ps.q8 ? q8_row_units(pool->cfg) : 0;
+  p.row_subs = p.row_units / pool->cfg.num_kv_heads;
+  p.row_recip = 65536 / (pool->cfg.num_heads / pool->cfg.num_kv_heads) + 1;
   p.q = (const uint16_t*)dev_q;
   p.out = (uint16_t*)dev_out;
   p.bt_off = (const int32_t*)(ws + ps.off_bt_off);
@@ -1186,15 +1232,22 @@ static int launch_attention(ic_pool* pool, const PlanSizes& ps, float scale, con
     // 8: tile kernel first 0.437 ms a call, rows first 0.495; 256 rows and 16 chunks of 2048 on 16384, 32 heads: 9.32 against
     // 9.52 ms.  A tile kernel that leads also asks for issue priority: what it loses to its neighbour's waves is lost to the
     // call (the same calls without: 0.441 and 9.35 ms, hardly more than runs differ).
-    const bool tile_main = ps.tile_leads;
+    // 8-bit pools: the tile kernel always leads, and the issue priority goes to the longer of the two: 128 rows and 8 chunks of 512, 40 heads
+    // (rows 420 us alone, tiles 260): rows 575 us a call, tiles 600; 64 heads over 8 (95 and 410): rows 478, tiles 455.
+    const bool tile_main = ps.q8 || ps.tile_leads;
     hipStream_t s_tile = tile_main ? st : pool->side, s_rows = tile_main ? pool->side : st;
-    p.tile_first = tile_main;
+    p.tile_first = ps.tile_leads;
     bool ok = true;
     auto run_tile = [&] {
       ProfScope ps_(pool, IC_K_TILE, s_tile);
-      ok = launch_tile_persist(p, D, pool->num_cus, true, s_tile) == hipSuccess;
+      ok = (ps.q8 ? launch_q8_tile(p, D, pool->cfg.dtype, pool->num_cus, s_tile) : launch_tile_persist(p, D, pool->num_cus, true, s_tile)) == hipSuccess;
     };
     auto run_rows = [&] {
+      if (ok && ps.q8) {
+        ProfScope ps_(pool, IC_K_GROUP, s_rows);
+        ok = launch_q8_rows(p, D, pool->cfg.dtype, true, s_rows) == hipSuccess;
+        return;
+      }
       if (ok && how.group == IC_LAUNCH_SLIM) {
         ProfScope ps_(pool, IC_K_GROUP, s_rows);
         ok = launch_group_slim(p, D, row_slots, s_rows) == hipSuccess;
@@ -1227,7 +1280,7 @@ static int launch_attention(ic_pool* pool, const PlanSizes& ps, float scale, con
     }
     if (how.group != IC_LAUNCH_NONE) {
       ProfScope ps_(pool, IC_K_GROUP, st);
-      if (launch_q8_rows(p, D, pool->cfg.dtype, st) != hipSuccess) return IC_EHIP;
+      if (launch_q8_rows(p, D, pool->cfg.dtype, how.group == IC_LAUNCH_SLIM, st) != hipSuccess) return IC_EHIP;
     }
   } else {
     if (how.tile != IC_LAUNCH_NONE) {

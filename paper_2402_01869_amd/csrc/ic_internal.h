@@ -96,7 +96,9 @@ struct AttnParams {
   int32_t merge_first;     // merge items [merge_first, merge_first + n_merge_items) are the merge kernel's
   int32_t n_merge_items;
   int32_t split_units;     // units of a split decode row merged by its last partition (heads, or K/V heads on the group kernel); 0: none is
-  int32_t row_units;       // 8-bit pools: workgroups per row item (K/V heads x 16-head parts of a group)
+  int32_t row_units;       // 8-bit pools: workgroups per row item, K/V heads x row_subs
+  int32_t row_subs;        // parts of at most 16 heads of a group
+  int32_t row_recip;       // c * row_recip >> 16 is c / group for c < 16
   float scale_log2e;       // scale * log2(e): scores are kept in log2 units
   int32_t row_variant;     // row-kernel build: bit0 = prefetch depth 2, bit1 = plain (cached) loads
   int32_t tile_first;      // persistent tile kernel: its waves ask for issue priority over the kernel beside it
@@ -163,7 +165,7 @@ hipError_t launch_group_slim(const AttnParams& p, int head_dim, int slots, hipSt
 hipError_t launch_append(void* pool, const void* k_new, const void* v_new, const int32_t* dev_dst, int32_t rows,
                          int num_heads, int head_dim, hipStream_t st);
 // The 8-bit pools' kernels; dtype: IC_DTYPE_E4M3 or IC_DTYPE_INT8.
-hipError_t launch_q8_rows(const AttnParams& p, int head_dim, int dtype, hipStream_t st);  // row items x row_units
+hipError_t launch_q8_rows(const AttnParams& p, int head_dim, int dtype, bool slim, hipStream_t st);  // row items x row_units; slim: head_dim <= 128
 hipError_t launch_q8_tile(const AttnParams& p, int head_dim, int dtype, int slots, hipStream_t st);
 hipError_t launch_q8_write(void* pool, size_t block_bytes, int dtype, const void* k_new, const void* v_new, const int32_t* dev_dst, int32_t rows,
                            int num_heads, int head_dim, hipStream_t st);

@@ -28,11 +28,10 @@ typedef __attribute__((ext_vector_type(2))) short s16x2;
 constexpr int kE4m3 = IC_DTYPE_E4M3, kInt8 = IC_DTYPE_INT8;
 constexpr uint32_t kNanBf16x2 = 0x7fc07fc0u;
 
-// 2^(b - 127) for the scale byte at bits 8 k .. 8 k + 7 of x; infinity for 255.
+// 2^(b - 127) for scale byte K of x; infinity for 255.  (One shift that selects its byte.)
 template <int K>
 __device__ __forceinline__ float scale_of(uint32_t x) {
-  constexpr int up = 23 - 8 * K;
-  return __builtin_bit_cast(float, (up >= 0 ? x << (up & 31) : x >> (-up & 31)) & 0x7f800000u);
+  return __builtin_bit_cast(float, ((x >> (8 * K)) & 0xffu) << 23);
 }
 
 // Two codes of x as bf16: bytes 0 and 1 (kHigh: 2 and 3).  Exact.

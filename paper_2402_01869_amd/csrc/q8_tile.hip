@@ -41,9 +41,10 @@ __host__ __device__ inline uint32_t q8_tile_round(const AttnParams& p) {
 // head group), which read the same keys, run on one L2 at the same time; fewer than 8 head groups: one shared queue (as the bf16
 // pools' persistent kernel).  The first round goes by index.
 template <int D, int FMT>
-__global__ __launch_bounds__((Impl8<D, FMT>::kThreads), 2) void q8_tile_kernel(AttnParams p) {
+__global__ __launch_bounds__((Impl8<D, FMT>::kThreads), 2) __attribute__((amdgpu_num_vgpr(104))) void q8_tile_kernel(AttnParams p) {
   __shared__ __attribute__((aligned(1024))) uint16_t lds[Impl8<D, FMT>::kLdsBytes / 2];
   __shared__ int s_next;
+  if (p.tile_first) __builtin_amdgcn_s_setprio(3);
   const uint32_t H = (uint32_t)p.num_heads >> p.tile_g_shift;  // head groups
   const bool per_xcd = H >= 8;
   const uint32_t x = blockIdx.x & 7u;

@@ -189,7 +189,8 @@ def test_decode_rows(fmt, H, Hkv, D, part):
 
 @FMT
 @pytest.mark.parametrize("H,Hkv,D", [(4, 4, 64), (3, 3, 128), (2, 2, 256), (6, 2, 128), (16, 2, 128), (8, 1, 256), (32, 1, 128)])
-@pytest.mark.parametrize("tuning", [dict(), dict(span_part_tokens=64, decode_part_tokens=64), dict(span_kernel=1), dict(span_kernel=2), dict(mfma_min_keys=1)])
+@pytest.mark.parametrize("tuning", [dict(), dict(span_part_tokens=64, decode_part_tokens=64), dict(span_kernel=1), dict(span_kernel=2), dict(mfma_min_keys=1),
+                                    dict(row_launch=3), dict(row_launch=2, decode_part_tokens=64, span_part_tokens=64), dict(serial_spans=1)])
 def test_chunks_and_decode_rows(fmt, H, Hkv, D, tuning):
     ctx = [70, 2, 40, 300, 64, 200, 333, 130, 5, 90]
     q_len = [1, 2, 40, 130, 33, 3, 70, 17, 1, 31]
@@ -203,6 +204,41 @@ def test_chunks_and_decode_rows(fmt, H, Hkv, D, tuning):
     got = _run(pool, batch, q)
     _close(got, *R.attention(pool_bytes, batch, q, Hkv, fmt), weights=ROWS_ONLY if tuning.get("span_kernel") == 1 else 2.0 ** -8)
     assert np.array_equal(got, _run(pool, batch, q))
+    pool.close()
+
+
+@FMT
+@pytest.mark.parametrize("H,Hkv,D,n", [(8, 8, 128, 40), (8, 8, 64, 40), (16, 2, 128, 60)])
+def test_rows_and_tiles_side_by_side(fmt, H, Hkv, D, n):
+    """The pair of kernels as a plan of its own choice, again and again from one plan: more work items than places."""
+    rng = np.random.default_rng(17)
+    ctx = list(rng.integers(100, 900, n)) + [400, 600, 300]
+    q_len = [1] * n + [300, 520, 100]
+    blocks = sum(-(-int(c) // 16) for c in ctx) + 5
+    batch = W.assemble_batch(H, D, 16, blocks, ctx, q_len, rng, num_kv_heads=Hkv)
+    pool_bytes = R.random_pool(batch, Hkv, D, fmt, rng)
+    q = W.randn_bf16((sum(q_len), H, D), rng)
+    pool, _ = _pool(pool_bytes, H, Hkv, D, fmt)
+    want = R.attention(pool_bytes, batch, q, Hkv, fmt)
+    pool.set_tuning(serial_spans=1)
+    alone = _run(pool, batch, q)
+    _close(alone, *want)
+    pool.set_tuning(row_launch=2)
+    desc = B.HostDesc.from_batch(batch)
+    assert pool.plan_image(desc)["side_by_side"] == 1
+    qt, ws = to_dev_bits(q), torch.empty(pool.workspace_bytes(desc), dtype=torch.uint8, device=DEV)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    plan = pool.plan_create(desc, ws.data_ptr(), ws.numel(), st.cuda_stream)
+    outs = [torch.zeros((len(q), H, D), dtype=torch.int16, device=DEV) for _ in range(4)]
+    torch.cuda.synchronize()
+    for out in outs:
+        pool.paged_attn_planned(plan, qt.data_ptr(), out.data_ptr(), st.cuda_stream)
+    st.synchronize()
+    for out in outs:
+        assert torch.equal(out, outs[0])
+    _close(from_dev_bits(outs[0]), *want)
+    plan.close()
     pool.close()
 
 
