@@ -624,18 +624,21 @@ void plan_sizes(const ic_pool* pool, const ic_batch_desc* d, PlanSizes& ps, Room
     const double tiles_time = t.serial_spans ? 0.0 : tile_load_us(pool, d, ps, &tiles_alone);
     if (ps.q8) {
       ps.row_part = part_alone;
-      // Side by side where the shorter of the two is expected to take at least kQ8Pair us: fork, join and the slower pace of both cost
-      // some 20 us and 0.45 of the shorter one's time.  Measured, one after the other / side by side: rows 420 and tiles 260 us
-      // 667 / 575, 95 and 410 490 / 455, 70 and 57 143 / 131, 1484 and 8314 9650 / 9211.  head_dim 256: two workgroups do not fit a CU.
+      // Side by side costs a fork and a join (13 us) and slows both.  Where the tiles take longer the rows ride along almost free, where the
+      // rows do, their kernel is one workgroup a CU beside a tile workgroup.  Over 145 batches (4 to 64 heads over 4 to 40 of 64 and 128 dims, 2
+      // to 200 decode rows of up to 6000 keys, 1 to 12 chunks of up to 1024 rows) these lines choose 0.8 % more than the better of
+      // the two in the mean and 14 % at most (always one after the other 2.5 % and 22 %).  Measured, one after the other / side by
+      // side: rows 420 and tiles 260 us alone 667 / 575, 95 and 410 490 / 455, 70 and 57 143 / 131, 1484 and 8314 9650 / 9211.
+      // head_dim 256: the two workgroups do not fit a CU.
       double bytes = 0.0;
       for (int s = 0; s < d->num_seqs; ++s) {
         const SeqRoute rt = route(ps, d->ctx_len[s], d->q_len[s]);
         if (rt.rest_rows) bytes += (double)((d->q_len[s] + ps.item_rows - 1) / ps.item_rows) * d->ctx_len[s] * q8_row_units(pool->cfg) * 2.0 * (pool->cfg.head_dim + 1);
       }
       const double rows_time = bytes / 6.4e6;
-      constexpr double kQ8Pair = 40.0;
+      const bool pays = tiles_time > rows_time ? rows_time > 12.0 : tiles_time > 25.0;
       ps.side_by_side = !t.serial_spans && pool->cfg.head_dim <= 128 && tiles_time > 0.0 && rows_time > 0.0 &&
-                        (t.row_launch >= 2 || std::min(tiles_time, rows_time) > kQ8Pair);
+                        (t.row_launch >= 2 || pays);
       ps.tile_leads = tiles_time > rows_time;
     } else if (tiles_time > 0.0 || (few_units && !t.serial_spans)) {
       RowLoad rows = row_load(pool, d, ps, ps.row_part);
