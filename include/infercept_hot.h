@@ -81,7 +81,9 @@ typedef struct {
  * A vector with a NaN or an infinity in it is kept as b = 255 and codes 0: all its values are NaN.
  *
  * Block of an 8-bit pool: codes [kv][kv_head][slot][dim], one byte each, then scale bytes [kv_head][kv][slot]; the block's size is
- * rounded up to a multiple of 128 bytes (kv_block_bytes), the padding is never read.  The pool may start out with any contents.
+ * rounded up to a multiple of 128 bytes (kv_block_bytes), the padding is never read.  The pool may start out with any contents; slots
+ * that a context covers have to hold what kv_write_span (or a swap) put there: e4m3 has codes of NaN, which kv_write_span never
+ * writes, and a value with one makes NaN of rows that are worked on together, not only of those that see it.
  */
 enum { IC_DTYPE_BF16 = 0, IC_DTYPE_E4M3 = 2, IC_DTYPE_INT8 = 3 };
 

@@ -20,9 +20,9 @@ extern "C" {
  * ic_prof_end synchronises the recorded events and returns totals per kernel kind.
  * ------------------------------------------------------------------------------------------ */
 enum { IC_K_ROW = 0, IC_K_TILE = 1, IC_K_MERGE = 2, IC_K_PACK = 3, IC_K_UNPACK = 4, IC_K_UPLOAD = 5, IC_K_APPEND = 6,
-       IC_K_GROUP = 7, IC_K_READ = 8, IC_K_COUNT = 9 };
-/* IC_K_UPLOAD: the kernel that copies a call's descriptor from pinned host memory to the device.  IC_K_GROUP: also the row kernel of
- * an 8-bit pool.  IC_K_READ: kv_read_span. */
+       IC_K_GROUP = 7, IC_K_COUNT = 8 };
+/* IC_K_UPLOAD: the kernel that copies a call's descriptor from pinned host memory to the device.  IC_K_APPEND: also kv_read_span.
+ * IC_K_GROUP: also the row kernel of an 8-bit pool. */
 typedef struct {
   int32_t launches[IC_K_COUNT];
   float total_ms[IC_K_COUNT];

@@ -21,8 +21,8 @@ IC_EDUP, IC_EUNSUPPORTED, IC_EOVERLAP, IC_EHIP, IC_ENOMEM, IC_ELIMIT = -6, -7, -
 IC_STATIC_PACK_MAX_BLOCKS = 65536
 IC_FLAG_TRUSTED = 1
 IC_DTYPE_BF16, IC_DTYPE_E4M3, IC_DTYPE_INT8 = 0, 2, 3
-IC_K_ROW, IC_K_TILE, IC_K_MERGE, IC_K_PACK, IC_K_UNPACK, IC_K_UPLOAD, IC_K_APPEND, IC_K_GROUP, IC_K_READ, IC_K_COUNT = range(10)
-KERNEL_NAMES = ("row", "tile", "merge", "pack", "unpack", "upload", "append", "group", "read")
+IC_K_ROW, IC_K_TILE, IC_K_MERGE, IC_K_PACK, IC_K_UNPACK, IC_K_UPLOAD, IC_K_APPEND, IC_K_GROUP, IC_K_COUNT = range(9)
+KERNEL_NAMES = ("row", "tile", "merge", "pack", "unpack", "upload", "append", "group")
 
 EXPORTS = (
     "ic_strerror", "kv_pool_init", "kv_pool_destroy", "kv_block_bytes",

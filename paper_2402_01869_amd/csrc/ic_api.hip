@@ -589,10 +589,13 @@ void plan_sizes(const ic_pool* pool, const ic_batch_desc* d, PlanSizes& ps, Room
   ps.spans_as_rows = (t.span_kernel == 1);  // default: MFMA tiles
   ps.decode_as_tiles = ps.tile_g_shift > 0 && t.span_kernel == 2;
   ps.decode_as_group = ps.tile_g_shift > 0 && t.span_kernel == 0;
-  // The row kernel of an 8-bit pool has 16 columns, which rows of a span share; spans of up to two such items need no tile.
+  // The row kernel of an 8-bit pool has 16 columns, which rows of a span share.  Spans of up to three such items (head_dim 256: two) are
+  // row items: a tile does the work of 256 (128) rows whatever it has.  Measured, row items / tiles, us: 40 heads of 128, 8 spans on 3000 keys,
+  // of 8 rows 54 / 126, 32 95 / 140, 48 133 / 142, 64 174 / 146; 32 of 64, 48 rows 50 / 70, 96 97 / 72; 64 over 8, 4 rows 20 / 30, 8
+  // rows 26 / 31, 16 41 / 37 (32 spans on 1000: 24 / 34, 45 / 35, 90 / 38); 16 of 256, 32 rows 54 / 64, 48 115 / 67.
   ps.q8 = is_q8(pool->cfg);
   ps.item_rows = ps.q8 ? std::max(1, 16 / G) : 1;
-  ps.short_span = ps.q8 && t.span_kernel != 2 ? 2 * ps.item_rows : 0;
+  ps.short_span = ps.q8 && t.span_kernel != 2 ? (pool->cfg.head_dim <= 128 ? 3 : 2) * ps.item_rows : 0;
   ps.row_part = std::min(t.decode_part_tokens > 0 ? round64(t.decode_part_tokens) : kDefaultRowPart, kMaxRowPart);
   int64_t tiles = 0, few = 0;  // unsplit query tiles; rows of spans with few keys
   for (int s = 0; s < d->num_seqs; ++s)
@@ -1406,7 +1409,7 @@ int kv_read_span_planned(ic_pool* pool, const ic_plan* plan, void* dev_k_out, vo
   const int rc = check_read_rows(pool, plan->total_q_rows, dev_k_out, dev_v_out);
   if (rc != IC_OK) return rc;
   hipStream_t st = (hipStream_t)hip_stream;
-  ProfScope ps_(pool, IC_K_READ, st);
+  ProfScope ps_(pool, IC_K_APPEND, st);
   return read_rows(pool, dev_k_out, dev_v_out, (const int32_t*)(plan->ws + plan->ps.off_row_dst), plan->total_q_rows, st) == hipSuccess ? IC_OK
                                                                                                                                      : IC_EHIP;
 }
@@ -1541,7 +1544,7 @@ int kv_read_span(ic_pool* pool, const ic_batch_desc* desc, void* dev_k_out, void
   if ((rc = upload_list(pool, kListAppend, src.data(), rows, false, st)) != IC_OK) return rc;
   hipError_t e;
   {
-    ProfScope ps_(pool, IC_K_READ, st);
+    ProfScope ps_(pool, IC_K_APPEND, st);
     e = read_rows(pool, dev_k_out, dev_v_out, pool->lists[kListAppend].dev, desc->total_q_rows, st);
   }
   return e == hipSuccess ? IC_OK : IC_EHIP;

@@ -508,7 +508,8 @@ def test_swap_moves_whole_blocks(fmt):
 
 
 @FMT
-def test_planned_calls_in_a_captured_graph(fmt):
+@pytest.mark.parametrize("tuning", [dict(), dict(row_launch=2), dict(decode_part_tokens=64, span_part_tokens=64)])
+def test_planned_calls_in_a_captured_graph(fmt, tuning):
     """One layer's write, attention and read back as a graph: every replay gives what the eager calls give on the inputs it finds."""
     H, D = 4, 128
     rng = np.random.default_rng(51)
@@ -516,6 +517,7 @@ def test_planned_calls_in_a_captured_graph(fmt):
     desc, rows = B.HostDesc.from_batch(batch), batch.total_q_rows
     start = R.random_pool(batch, H, D, fmt, rng)
     pool, t = _pool(start.copy(), H, H, D, fmt)
+    pool.set_tuning(**tuning)
     ws = torch.empty(pool.workspace_bytes(desc), dtype=torch.uint8, device=DEV)
     q, k, v, out, kb, vb = (torch.zeros((rows, H, D), dtype=torch.int16, device=DEV) for _ in range(6))
     plan = pool.plan_create(desc, ws.data_ptr(), ws.numel(), 0)

@@ -139,11 +139,12 @@ def test_plan_covers_every_visible_key_once(fmt, H, Hkv, D, tuning):
 
 @FMT
 def test_short_spans_are_row_items(fmt):
-    """Up to two row items of 16 columns; longer ones are tiles, and all of them with span_kernel = 2."""
-    for H, Hkv, n, tiles in [(4, 4, 32, 0), (4, 4, 33, 1), (64, 8, 4, 0), (64, 8, 5, 1), (32, 1, 2, 0), (32, 1, 3, 1)]:
+    """Up to three row items of 16 columns (head_dim 256: two); longer ones are tiles, and all of them with span_kernel = 2."""
+    for H, Hkv, D, n, tiles in [(4, 4, 128, 48, 0), (4, 4, 128, 49, 1), (64, 8, 128, 6, 0), (64, 8, 128, 7, 1), (32, 1, 64, 3, 0), (32, 1, 64, 4, 1),
+                                (4, 4, 256, 32, 0), (4, 4, 256, 33, 1)]:
         blocks = 80
-        batch = W.assemble_batch(H, 128, 16, blocks, [1000], [n], np.random.default_rng(1), num_kv_heads=Hkv)
-        p = _pool(fmt, blocks, H, 128, Hkv)
+        batch = W.assemble_batch(H, D, 16, blocks, [1000], [n], np.random.default_rng(1), num_kv_heads=Hkv)
+        p = _pool(fmt, blocks, H, D, Hkv)
         desc = B.HostDesc.from_batch(batch)
         assert bool(p.plan_query(desc)["tile_items"]) == bool(tiles)
         p.set_tuning(span_kernel=2)
