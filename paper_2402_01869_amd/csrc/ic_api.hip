@@ -1185,7 +1185,7 @@ static int launch_attention(ic_pool* pool, const PlanSizes& ps, float scale, con
   }
   AttnParams p;
   p.pool = (const uint16_t*)pool->base;
-  p.block_bytes = pool->block_bytes;
+  p.block_bytes = (uint32_t)pool->block_bytes;  // 8-bit pools: at most 2 * 4096 * 16 * 257 bytes
   p.row_units = ps.q8 ? q8_row_units(pool->cfg) : 0;
   p.row_subs = p.row_units / pool->cfg.num_kv_heads;
   p.row_recip = 65536 / (pool->cfg.num_heads / pool->cfg.num_kv_heads) + 1;

@@ -70,7 +70,7 @@ struct MergeItem {
 
 struct AttnParams {
   const uint16_t* pool;    // bf16 pools: the cache; 8-bit pools: base of the blocks
-  uint64_t block_bytes;
+  uint32_t block_bytes;
   const uint16_t* q;
   uint16_t* out;
   const int32_t* bt_off;   // [num_seqs] offset of each sequence's ids in bt_flat

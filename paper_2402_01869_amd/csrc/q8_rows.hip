@@ -264,12 +264,11 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
   uint32_t v_off = (uint32_t)(Hk + kvh) * R::kTile + (lane ^ swap_v<D>(lane / kCh)) * 16u;
   uint32_t s_off = 2u * Hk * R::kTile + (uint32_t)kvh * 2u * kBlockSize + 4u * (lane & 7);
   const char* const pool = (const char*)p.pool;
-  const uint64_t block_bytes = p.block_bytes;
-  const auto fetch = [&](auto k_tag, auto v_tag, int tile, uint32_t at) __attribute__((always_inline)) {
-    const int b0 = it.k_begin / kBlockSize + 2 * tile;
+  const uint32_t block_bytes = p.block_bytes;
+  const auto fetch = [&](auto k_tag, auto v_tag, int id0, int id1, uint32_t at) __attribute__((always_inline)) {
     constexpr bool kDoK = decltype(k_tag)::value, kDoV = decltype(v_tag)::value;
     if constexpr (kSlim) asm volatile("" : "+v"(k_off), "+v"(v_off));  // what is derived from them is worked out here, not kept
-    const char* const base[2] = {pool + (uint64_t)(uint32_t)bt[b0] * block_bytes, pool + (uint64_t)(uint32_t)bt[min(b0 + 1, last_blk)] * block_bytes};
+    const char* const base[2] = {pool + (uint64_t)(uint32_t)id0 * block_bytes, pool + (uint64_t)(uint32_t)id1 * block_bytes};
     uint32_t k[kParts], v[kParts];
 #pragma unroll
     for (int i = 0; i < kParts; ++i) {
@@ -394,7 +393,8 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
       const uint32_t vb = vsc[i / 4];
       const float a = p0 * (i % 4 == 0 ? scale_of<0>(vb) : scale_of<2>(vb)), b = p1 * (i % 4 == 0 ? scale_of<1>(vb) : scale_of<3>(vb));
       const bf16x2 h = {(__bf16)a, (__bf16)b};
-      const uint32_t hb = __builtin_bit_cast(uint32_t, h);
+      uint32_t hb = __builtin_bit_cast(uint32_t, h);
+      asm("" : "+v"(hb));  // the halves are taken from the pair, not rounded again
       const bf16x2 r = {(__bf16)(a - __builtin_bit_cast(float, hb << 16)), (__bf16)(b - __builtin_bit_cast(float, hb & 0xffff0000u))};
       hi[i / 2] = hb;
       lo[i / 2] = __builtin_bit_cast(uint32_t, r);
@@ -424,7 +424,12 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
   };
 
   // Q and the first tiles are asked for together; from the wait for Q on, no load but copies is in flight.
-  for (int i = 0; i < R::kStages && i < n_mine; ++i) fetch(yes, yes, w + kWaves * i, ring_at + i * R::kStage);
+  const int blk0 = it.k_begin / kBlockSize + 2 * w;
+  const auto block = [&](int i, int b) { return bt[min(blk0 + 2 * kWaves * i + b, last_blk)]; };  // of this wave's tile i
+  for (int i = 0; i < R::kStages && i < n_mine; ++i) fetch(yes, yes, block(i, 0), block(i, 1), ring_at + i * R::kStage);
+  // Ids of the tile that is asked for next, loaded an iteration ahead (waited for where they are used: 8 rows of 1000..8000 keys, 64 heads
+  // over 8, plan and 4 layers 102 -> 100 us; 128 rows beside 8 chunks, 40 heads, 582 -> 575).
+  int id0 = block(R::kStages, 0), id1 = block(R::kStages, 1);
 #pragma unroll
   for (int j = 0; j < 2 * R::kKL; ++j) asm volatile("" ::"v"(q[j]));
   if constexpr (kSlim) {
@@ -444,7 +449,9 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
       step(w + kWaves * i, at, [] {}, [] {});
       if (i + R::kStages < n_mine) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage has been read
-        fetch(yes, yes, w + kWaves * (i + R::kStages), ring_at + at);
+        fetch(yes, yes, id0, id1, ring_at + at);
+        id0 = block(i + 1 + R::kStages, 0);
+        id1 = block(i + 1 + R::kStages, 1);
       }
       at = at + R::kStage == (uint32_t)R::kWaveLds ? 0u : at + R::kStage;
     }
@@ -456,14 +463,16 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
           w + kWaves * i, 0u,
           [&]() __attribute__((always_inline)) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (more) fetch(yes, no, w + kWaves * (i + 1), ring_at);
+            if (more) fetch(yes, no, id0, id1, ring_at);
           },
           [&]() __attribute__((always_inline)) {
             if (more) wait_copies<R::kCopiesK>();
             else wait_copies<0>();
           });
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (more) fetch(no, yes, w + kWaves * (i + 1), ring_at);
+      if (more) fetch(no, yes, id0, id1, ring_at);
+      id0 = block(i + 2, 0);
+      id1 = block(i + 2, 1);
     }
   }
 

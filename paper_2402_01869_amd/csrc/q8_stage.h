@@ -20,7 +20,7 @@ struct Codes {
 template <int D, int FMT>
 struct Stager {
   const char* pool;      // base of the pool
-  uint64_t block_bytes;
+  uint32_t block_bytes;
   uint32_t code_at[2];   // this lane's codes of K and of V, and
   uint32_t scale_at;     // ... its key's scale byte, inside a block
   uint32_t lds_at;       // this lane's first 16 bytes among the wave's 8 keys of a staged tile
