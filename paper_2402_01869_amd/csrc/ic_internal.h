@@ -69,8 +69,7 @@ struct MergeItem {
 };
 
 struct AttnParams {
-  const uint16_t* pool;    // bf16 pools: the cache; 8-bit pools: base of the blocks
-  uint32_t block_bytes;
+  const uint16_t* pool;    // base of the blocks
   const uint16_t* q;
   uint16_t* out;
   const int32_t* bt_off;   // [num_seqs] offset of each sequence's ids in bt_flat
@@ -96,13 +95,15 @@ struct AttnParams {
   int32_t merge_first;     // merge items [merge_first, merge_first + n_merge_items) are the merge kernel's
   int32_t n_merge_items;
   int32_t split_units;     // units of a split decode row merged by its last partition (heads, or K/V heads on the group kernel); 0: none is
-  int32_t row_units;       // 8-bit pools: workgroups per row item, K/V heads x row_subs
-  int32_t row_subs;        // parts of at most 16 heads of a group
-  int32_t row_recip;       // c * row_recip >> 16 is c / group for c < 16
   float scale_log2e;       // scale * log2(e): scores are kept in log2 units
   int32_t row_variant;     // row-kernel build: bit0 = prefetch depth 2, bit1 = plain (cached) loads
   int32_t tile_first;      // persistent tile kernel: its waves ask for issue priority over the kernel beside it
   int32_t* counters;       // 16 work-queue counters, zero when the kernel starts
+  // 8-bit pools
+  uint32_t block_bytes;
+  int32_t row_units;       // workgroups per row item, K/V heads x row_subs
+  int32_t row_subs;        // parts of at most 16 heads of a group
+  int32_t row_recip;       // c * row_recip >> 16 is c / group for c < 16
 };
 
 // Where a sequence's ids begin, for the tile kernels' work items.  The offsets of the first 64 sequences are loaded one per lane (the

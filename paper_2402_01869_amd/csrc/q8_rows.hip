@@ -127,7 +127,7 @@ __device__ __forceinline__ f32x4 mfma(const bf16x8 a, const bf16x8 b, const f32x
 // End of a partition of a split decode row: as mergep::finish_split (the workgroup that finds the others' partial results there merges
 // them, in an order that does not depend on who is last), but with all 256 threads.  The row's heads x D values are few for one head, and a
 // thread that reads all partitions of its own waits for memory once per batch of them: here a thread has four values of every
-// kSets-th partition, and the sets meet in LDS.
+// sets-th partition, and the sets meet in LDS.
 template <int D>
 __device__ __forceinline__ void finish_row(const AttnParams& p, int slot, int unit, int head0, int heads, float* lds, int* s_last) {
   using mergep::f32x2;

@@ -255,7 +255,8 @@ __device__ __forceinline__ void tile16_body(const AttnParams& p, const TileItem&
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
 
-  const int n_half = wave_pos_hi < it.k_begin ? 0 : min(2 * n_tiles, (wave_pos_hi - it.k_begin) / 32 + 1);  // halves this wave sees
+  // (8-bit pools: a wave without a row of its own brings in its keys and meets the others, and computes nothing)
+  const int n_half = wave_pos_hi < it.k_begin || (kQ8 && kRows * w >= n_rows_t) ? 0 : min(2 * n_tiles, (wave_pos_hi - it.k_begin) / 32 + 1);  // halves this wave sees
   u32x4 kop[kQ];    // K operands; the first four are read at the end of the stage before
   bf16x8 vop[kP];   // V operands
   auto must_move = [&]() { return __builtin_amdgcn_ballot_w64(top * sc > m + kLazyLog2) != 0; };

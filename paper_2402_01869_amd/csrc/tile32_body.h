@@ -363,7 +363,8 @@ __device__ __forceinline__ void tile32_body(const AttnParams& p, const TileItem&
   // Both start from the scores of half 2 u - 1 (sb) and the weights of half 2 u - 2 (pa) and leave those of the next tile.  The serial step
   // does the first and the last tiles, hidden keys and all; there is one copy of it, for a call on a few tiles is over before
   // more code has been fetched.
-  const int n_half = wave_pos_hi < it.k_begin ? 0 : min(2 * n_tiles, (wave_pos_hi - it.k_begin) / 32 + 1);  // halves this wave sees
+  // (8-bit pools: a wave without a row of its own brings in its keys and meets the others, and computes nothing)
+  const int n_half = wave_pos_hi < it.k_begin || (kQ8 && 32 * w >= n_rows_t) ? 0 : min(2 * n_tiles, (wave_pos_hi - it.k_begin) / 32 + 1);  // halves this wave sees
   u32x4 kop[kQ];    // K operands; the first two are read at the end of the stage before
   bf16x8 vop[kP];   // V operands
   auto must_move = [&]() { return __builtin_amdgcn_ballot_w64(!(top * sc <= m + kLazyLog2)) != 0; };
