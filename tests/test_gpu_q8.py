@@ -577,3 +577,66 @@ def test_pools_on_two_streams_do_not_meet(fmt):
     for pool, _, _, _, out, _, _, want in runs:
         _close(from_dev_bits(out), *want)
         pool.close()
+
+
+@FMT
+def test_more_row_items_than_one_grid_dimension(fmt):
+    """33000 sequences of one token: the result is that token's value (weight 1), to the bit."""
+    n, H, D = 33000, 2, 64
+    bb = B.block_bytes(1, D, 16, R.FORMATS[fmt])
+    pool = B.KvPool.from_tensor(torch.full((n, bb), 0xFF, dtype=torch.uint8, device=DEV), H, D, num_kv_heads=1, dtype=R.FORMATS[fmt])
+    rng = np.random.default_rng(21)
+    ids = rng.permutation(n).astype(np.int32)[:, None]
+    ones, start = np.ones(n, np.int32), np.arange(n, dtype=np.int32)
+    desc = B.HostDesc(ones, ones, start, ids, 0.125, n)
+    k, v = (to_dev_bits(W.randn_bf16((n, 1, D), rng)) for _ in range(2))
+    q, out, back = to_dev_bits(W.randn_bf16((n, H, D), rng)), torch.zeros((n, H, D), dtype=torch.int16, device=DEV), torch.zeros_like(v)
+    ws = torch.empty(pool.workspace_bytes(desc), dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    pool.kv_write_span(desc, k.data_ptr(), v.data_ptr())
+    pool.paged_attn_mixed(desc, q.data_ptr(), out.data_ptr(), ws.data_ptr(), ws.numel())
+    pool.kv_read_span(desc, k.data_ptr(), back.data_ptr())
+    torch.cuda.synchronize()
+    # (as numbers: a code of -0 comes out as 0)
+    assert np.array_equal(W.bf16_bits_to_f64(from_dev_bits(out)), np.broadcast_to(W.bf16_bits_to_f64(from_dev_bits(back)), (n, H, D)))
+    pool.close()
+
+
+@FMT
+@pytest.mark.parametrize("H,Hkv,D", [(2, 2, 64), (8, 2, 128), (1, 1, 256)])
+def test_query_rows_that_are_not_finite_stay_alone(fmt, H, Hkv, D):
+    """Columns of one row item and rows of one tile: a query of NaN or infinities is the NaN of its own row and head only."""
+    ctx, q_len = [300, 200, 70, 90, 33], [150, 1, 5, 64, 2]
+    rng = np.random.default_rng(31)
+    batch = W.assemble_batch(H, D, 16, 60, ctx, q_len, rng, num_kv_heads=Hkv)
+    pool_bytes = R.random_pool(batch, Hkv, D, fmt, rng)
+    q = W.randn_bf16((sum(q_len), H, D), rng)
+    want, dev = R.attention(pool_bytes, batch, q, Hkv, fmt)
+    bad = q.copy()
+    for i, r in enumerate((3, 100, 149, 150, 153, 170, 219, 221)):
+        bad[r, i % H, i::16] = (0x7FC0, 0x7F80, 0xFF80)[i % 3]   # NaN, inf, -inf
+        want[r, i % H] = np.nan
+    pool, _ = _pool(pool_bytes, H, Hkv, D, fmt)
+    for tuning in (dict(), dict(span_kernel=1), dict(span_part_tokens=64, decode_part_tokens=64), dict(row_launch=2)):
+        pool.set_tuning(**tuning)
+        got, fine = W.bf16_bits_to_f64(_run(pool, batch, bad)), ~np.isnan(want)
+        assert np.isnan(got[~fine]).all()
+        bound = (2.0 ** -8 + 1e-5) * np.abs(want) + (2.0 ** -8 + 1e-3) * dev + 1e-6
+        assert (np.abs(got - want)[fine] <= bound[fine]).all()
+    pool.close()
+
+
+@FMT
+def test_the_same_call_gives_the_same_bits(fmt):
+    """Partitions end in any order; rows split inside the row kernel, by the merge kernel, and beside tiles."""
+    rng = np.random.default_rng(41)
+    for H, Hkv, D, ctx, q_len in [(8, 8, 128, [5000, 900], [1, 1]), (8, 2, 64, [4700, 3000], [3, 1]), (8, 1, 128, [2500, 4200, 3100], [300, 1, 2])]:
+        batch = W.assemble_batch(H, D, 16, sum(ctx) // 16 + 8, ctx, q_len, rng, num_kv_heads=Hkv)
+        pool, _ = _pool(R.random_pool(batch, Hkv, D, fmt, rng), H, Hkv, D, fmt)
+        q = W.randn_bf16((sum(q_len), H, D), rng)
+        for tuning in (dict(), dict(decode_part_tokens=128, span_part_tokens=512), dict(row_launch=2)):
+            pool.set_tuning(**tuning)
+            first = _run(pool, batch, q)
+            for _ in range(6):
+                assert np.array_equal(_run(pool, batch, q), first)
+        pool.close()
