@@ -15,6 +15,10 @@
 //     dims in the order that falls out: row n of product (w, b) is dim n * D / 16 + 4 w + b.
 //   - Weights go in as two bf16 numbers (16 bits of significand; the rounding of one, 2^-9, would show in rows of a few keys): the
 //     matrix pipe has the time.  The normaliser is the fp32 sum of the unrounded weights, what is lost is 2^-17 of a weight.
+//     Items of up to 8 columns (kPair: decode rows of groups of up to 8 heads) have their first numbers in columns 0..7 and
+//     the second ones in 8..15: half the products, and one sum across lanes at the end.  Beside the tile kernel: 128 rows and 8
+//     chunks, 40 heads, 573 -> 568 us; alone, int8, 8 rows of 1000..3000 keys, 32 heads of 64, 21.2 -> 20.2 us, 200 of 600..1200, 40
+//     heads of 128, 293 -> 289, of 40..300 81 -> 82.5.
 // Keys a column does not see: score -inf, weight 0, and 0 for the scale of their value, which may be infinite (NaN vectors); codes
 // behind the item's last key are cleared, they may be anything (0 * NaN).
 #include <algorithm>
@@ -124,6 +128,11 @@ __device__ __forceinline__ f32x4 mfma(const bf16x8 a, const bf16x8 b, const f32x
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+// What the lane 8 on among 16 has.
+__device__ __forceinline__ float across(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x128, 0xf, 0xf, true));
+}
+
 // End of a partition of a split decode row: as mergep::finish_split (the workgroup that finds the others' partial results there merges
 // them, in an order that does not depend on who is last), but with all 256 threads.  The row's heads x D values are few for one head, and a
 // thread that reads all partitions of its own waits for memory once per batch of them: here a thread has four values of every
@@ -209,11 +218,11 @@ __device__ __forceinline__ void finish_row(const AttnParams& p, int slot, int un
 
 // kMerge: split decode rows are merged by their last partition, else by the merge kernel.
 // kSlim: Q^T stays in LDS behind the rings, which takes 16 registers less.
-template <int D, int FMT, bool kMerge, bool kSlim>
+// kPair: the item has at most 8 columns; lanes n and n + 8 share one.
+template <int D, int FMT, bool kMerge, bool kSlim, bool kPair>
 __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* s_last) {
   using R = R8<D>;
   const uint32_t item_idx = blockIdx.z * kGridItems + blockIdx.y;
-  if (item_idx >= (uint32_t)(p.n_row_items - p.group_first)) return;
   const int unit = (int)blockIdx.x;
   const RowItem it = p.row_items[p.group_first + item_idx];
   const int n_rows = it.pad[0], pos0 = it.pad[1], nparts = it.pad[2];
@@ -225,7 +234,7 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g = lane >> 4;
   const int cols = n_rows * heads;               // columns that are rows of the result, <= 16
-  const int col = min(n, cols - 1);              // the others mirror the last one
+  const int col = min(kPair ? n & 7 : n, cols - 1);  // the others mirror the last one
   const auto row_of = [&](int c) { return n_rows == 1 ? 0 : c * p.row_recip >> 16; };  // c / heads (several rows: all heads of the group)
   const int row = row_of(col), head = head0 + (col - row * heads);
   const int limit = min(pos0 + row + 1, it.k_end);  // keys the column sees are below
@@ -242,6 +251,8 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
       q[2 * j + 1] = *(const bf16x8*)(qp + 64 * j + 8);
     }
   }
+  const bool upper = (n & 8) != 0;
+  const float take = upper ? -1.0f : 0.0f;
   f32x4 o[R::kDT];
 #pragma unroll
   for (int i = 0; i < R::kDT; ++i) o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -385,7 +396,7 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
 #pragma unroll
       for (int i = 0; i < R::kDT; ++i) o[i] *= was;
     }
-    u32x4 hi, lo;
+    u32x4 hi, lo = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
       const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], sc, -m)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i + 1], sc, -m));
@@ -395,9 +406,16 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
       const bf16x2 h = {(__bf16)a, (__bf16)b};
       uint32_t hb = __builtin_bit_cast(uint32_t, h);
       asm("" : "+v"(hb));  // the halves are taken from the pair, not rounded again
-      const bf16x2 r = {(__bf16)(a - __builtin_bit_cast(float, hb << 16)), (__bf16)(b - __builtin_bit_cast(float, hb & 0xffff0000u))};
-      hi[i / 2] = hb;
-      lo[i / 2] = __builtin_bit_cast(uint32_t, r);
+      if constexpr (kPair) {
+        // lanes 0..7 take 0 off and round as before, the upper ones are left with the second number
+        const bf16x2 r = {(__bf16)__builtin_fmaf(take, __builtin_bit_cast(float, hb << 16), a),
+                          (__bf16)__builtin_fmaf(take, __builtin_bit_cast(float, hb & 0xffff0000u), b)};
+        hi[i / 2] = __builtin_bit_cast(uint32_t, r);
+      } else {
+        const bf16x2 r = {(__bf16)(a - __builtin_bit_cast(float, hb << 16)), (__bf16)(b - __builtin_bit_cast(float, hb & 0xffff0000u))};
+        hi[i / 2] = hb;
+        lo[i / 2] = __builtin_bit_cast(uint32_t, r);
+      }
     }
     const bf16x8 ph = __builtin_bit_cast(bf16x8, hi), pl = __builtin_bit_cast(bf16x8, lo);
     if constexpr (R::kStages == 1) {
@@ -416,10 +434,12 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
       o[4 * e + 1] = mfma(a1, ph, o[4 * e + 1]);
       o[4 * e + 2] = mfma(a2, ph, o[4 * e + 2]);
       o[4 * e + 3] = mfma(a3, ph, o[4 * e + 3]);
-      o[4 * e] = mfma(a0, pl, o[4 * e]);
-      o[4 * e + 1] = mfma(a1, pl, o[4 * e + 1]);
-      o[4 * e + 2] = mfma(a2, pl, o[4 * e + 2]);
-      o[4 * e + 3] = mfma(a3, pl, o[4 * e + 3]);
+      if constexpr (!kPair) {
+        o[4 * e] = mfma(a0, pl, o[4 * e]);
+        o[4 * e + 1] = mfma(a1, pl, o[4 * e + 1]);
+        o[4 * e + 2] = mfma(a2, pl, o[4 * e + 2]);
+        o[4 * e + 3] = mfma(a3, pl, o[4 * e + 3]);
+      }
     }
   };
 
@@ -482,6 +502,12 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
   const int ne = tid_e & 15, ge = (tid_e >> 4) & 3;
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
+  if constexpr (kPair) {
+#pragma unroll
+    for (int i = 0; i < R::kDT; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[i][r] += across(o[i][r]);
+  }
   float* const mine = lds + w * R::kSlice;
   if (ne < cols) {
 #pragma unroll
@@ -526,11 +552,20 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
   }
 }
 
+template <int D, int FMT, bool kMerge, bool kSlim>
+__device__ __forceinline__ void rows_any(const AttnParams& p, float* lds, int* s_last) {
+  const uint32_t item_idx = blockIdx.z * kGridItems + blockIdx.y;
+  if (item_idx >= (uint32_t)(p.n_row_items - p.group_first)) return;
+  const int heads = p.row_subs == 1 ? p.group : kCols;  // (the last part of a larger group may have fewer)
+  if (p.row_items[p.group_first + item_idx].pad[0] * heads <= 8) rows_body<D, FMT, kMerge, kSlim, true>(p, lds, s_last);
+  else rows_body<D, FMT, kMerge, kSlim, false>(p, lds, s_last);
+}
+
 template <int D, int FMT, bool kMerge>
 __global__ __launch_bounds__(64 * kWaves, 2) void q8_rows_kernel(AttnParams p) {
   __shared__ __attribute__((aligned(1024))) float lds[kWaves * R8<D>::kSlice];
   __shared__ int s_last;
-  rows_body<D, FMT, kMerge, false>(p, lds, &s_last);
+  rows_any<D, FMT, kMerge, false>(p, lds, &s_last);
 }
 
 // The build that runs beside the tile kernel (208 registers, two waves a SIMD): at most 96 registers, one of its waves a SIMD.  LDS is asked
@@ -543,7 +578,7 @@ template <int D, int FMT>
 __global__ __launch_bounds__(64 * kWaves, 5) void q8_rows_slim_kernel(AttnParams p) {
   extern __shared__ __attribute__((aligned(1024))) float slim_lds[];
   if (!p.tile_first) __builtin_amdgcn_s_setprio(3);
-  rows_body<D, FMT, false, true>(p, slim_lds, nullptr);
+  rows_any<D, FMT, false, true>(p, slim_lds, nullptr);
 }
 
 template <int D, int FMT>
