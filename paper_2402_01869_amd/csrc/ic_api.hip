@@ -631,7 +631,7 @@ void plan_sizes(const ic_pool* pool, const ic_batch_desc* d, PlanSizes& ps, Room
       // rows do, their kernel is one workgroup a CU beside a tile workgroup.  Over 145 batches (4 to 64 heads over 4 to 40 of 64 and 128 dims, 2
       // to 200 decode rows of up to 6000 keys, 1 to 12 chunks of up to 1024 rows) these lines choose 0.8 % more than the better of
       // the two in the mean and 14 % at most (always one after the other 2.5 % and 22 %).  Measured, one after the other / side by
-      // side: rows 420 and tiles 260 us alone 667 / 575, 95 and 410 490 / 455, 70 and 57 143 / 131, 1484 and 8314 9650 / 9211.
+      // side: rows 420 and tiles 260 us alone 671 / 568, 95 and 410 502 / 457, 70 and 57 137 / 124, 1484 and 8314 9740 / 9200.
       // head_dim 256: the two workgroups do not fit a CU.
       double bytes = 0.0;
       for (int s = 0; s < d->num_seqs; ++s) {
@@ -1239,7 +1239,7 @@ static int launch_attention(ic_pool* pool, const PlanSizes& ps, float scale, con
     // 9.52 ms.  A tile kernel that leads also asks for issue priority: what it loses to its neighbour's waves is lost to the
     // call (the same calls without: 0.441 and 9.35 ms, hardly more than runs differ).
     // 8-bit pools: the tile kernel always leads, and the issue priority goes to the longer of the two: 128 rows and 8 chunks of 512, 40 heads
-    // (rows 420 us alone, tiles 260): rows 575 us a call, tiles 600; 64 heads over 8 (95 and 410): rows 478, tiles 455.
+    // (rows 420 us alone, tiles 260): rows 576 us a call, tiles 591; 64 heads over 8 (95 and 410): rows 483, tiles 458.
     const bool tile_main = ps.q8 || ps.tile_leads;
     hipStream_t s_tile = tile_main ? st : pool->side, s_rows = tile_main ? pool->side : st;
     p.tile_first = ps.tile_leads;

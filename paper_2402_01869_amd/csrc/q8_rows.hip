@@ -1,6 +1,10 @@
 // Row kernel of the 8-bit cache: query rows that are few for their keys.  Decode rows of every pool (Section 4.2: one query token,
 // every cached vector read once), short chunks, and the rows of a fresh chunk that see fewer than 64 keys.
 //
+// Measured, GB/s of cached bytes, e4m3 / integers: 128 rows of 256..4096, 40 heads of 128, 6600 / 6560; 256 rows of 512..2048, 16 heads of 256, 6530 / 6560;
+// 128 rows, 32 heads of 64, 6170 / 6020; 64 heads over 8, 5910 / 5450.  Vector ALU 30 % (integers 45 %) and matrix pipe 9 % busy, no LDS
+// conflicts, 1.02 times the bytes fetched.  Beside the tile kernel, one workgroup a CU, the wait for memory is exposed: 4000 to 5000.
+//
 // One workgroup = one row item (up to 16 columns: consecutive query rows of a sequence x the query heads of a K/V head) x one K/V head,
 // 4 waves, wave w the item's 32-key tiles w, w + 4, ...  HBM-bound: a byte of the cache is read once and meets all columns.
 // Every wave copies its tiles from the pool straight into a ring of its own in LDS (no registers, no barrier), one or two tiles ahead, and codes

@@ -3,6 +3,12 @@
 // The expansion of a code, with its scale, to bf16 is exact (q8.h), so the tile is the bf16 pools' (tile32_body.h, head_dim 256
 // tile16_body.h): the same steps and the same arithmetic on the same numbers.  What differs is how a tile gets into LDS (q8_stage.h).
 // Rows that see fewer than 64 keys do not run here: the weights are rounded to bf16 (2^-9 each).
+//
+// Bound by the matrix pipe's issue and, on long chunks, by the power cap, as the bf16 kernel: converting a tile's codes once for its 256 (128)
+// rows is hidden between the products.  208 registers, two waves a SIMD, leave the 96 that a wave of the slim row kernel has beside them.
+// Measured alone, e4m3 / integers (two more instructions a pair of codes), TFLOP/s: 16 chunks of 2048 on 16384 keys, 32 heads of 128, 1120 / 1035;
+// 8 of 512 on 1024..4096, 64 heads over 8, 1020 / 975, 40 heads 835 / 785; 8 of 2048 on 8192, 16 heads of 256, 955 / 887; 8 of 1024 on 4096, 32
+// heads of 64, 835 / 780.
 #include <algorithm>
 
 #include "tile16_body.h"
