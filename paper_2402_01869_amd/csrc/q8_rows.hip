@@ -91,12 +91,12 @@ __device__ __forceinline__ void copy_block(const char* base, const uint32_t (&of
   if constexpr (N == 1)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1 nt" ::"s"(at), "s"(base), "v"(off[0]) : "memory", "m0");
   else if constexpr (N == 2)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1 nt\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024 nt" ::"s"(at),
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1 nt\n\tglobal_load_lds_dwordx4 %3, %1 offset:0x400 nt" ::"s"(at),
                  "s"(base), "v"(off[0]), "v"(off[1])
                  : "memory", "m0");
   else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1 nt\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024 nt\n\t"
-                 "global_load_lds_dwordx4 %4, %1 offset:2048 nt\n\tglobal_load_lds_dwordx4 %5, %1 offset:3072 nt" ::"s"(at),
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1 nt\n\tglobal_load_lds_dwordx4 %3, %1 offset:0x400 nt\n\t"
+                 "global_load_lds_dwordx4 %4, %1 offset:0x800 nt\n\tglobal_load_lds_dwordx4 %5, %1 offset:0xc00 nt" ::"s"(at),
                  "s"(base), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3])
                  : "memory", "m0");
 }
