@@ -193,6 +193,7 @@ struct PlanSizes {
   int tile_g_shift;                    // log2 of the query heads one tile workgroup serves
   bool q8;                             // an 8-bit pool: its row kernel takes all row items, several rows of a span to an item
   int item_rows;                       // query rows of a row item, at most (1 in a bf16 pool)
+  int alone_keys, row_long;            // whole row items of up to alone_keys keys are a wave's each; the number of the others, which come first
   int short_span;                      // spans of up to so many rows are row items (0 in a bf16 pool)
   bool spans_as_rows;
   bool few_as_units;                   // few-key rows of spans go to the tile kernels' few-key body
@@ -303,6 +304,15 @@ double side_by_side_us(const LaunchRates& rate, double tiles, const RowLoad& r) 
 double serial_us(const LaunchRates& rate, double tiles, const RowLoad& r, bool few_units) {
   return (few_units ? 17.5 : 24.5) + tiles + std::max(r.bytes / 6.2e6, r.longest / rate.row_alone);
 }
+
+// Row items of an 8-bit pool that a wave has alone, four to a workgroup: whole ones of up to so many keys, once they are more than the places of a
+// workgroup (two to a CU), and of up to twice as many keys once they are more than twice the places.  A workgroup begins and ends
+// in some 3 us, and on a few keys little else; one that has its place at once is done sooner when its four waves share the keys.
+// Measured, e4m3, in teams / alone, us: 40 heads, 1 row of 120 keys 4.0 / 5.7, 16 of 250 11.1 / 10.0, 64 of 125..250 29.8 / 24.3, of 250..500 52.2 / 45.1,
+// 256 of 30..60 64.5 / 30.1, of 250..500 173 / 159; 32 heads, 223 of 1..2 40.9 / 14.4; 64 over 8, 256 of 125..250 27.6 / 23.4; 16 of 256 dims, 256 of
+// 60..120 45.9 / 35.3; 8 fresh chunks of 300..800, 64 over 8, whose first 63 rows are such items beside the tiles, 111.6 / 98.2, one of 512, 40 heads (160
+// workgroups) 27.4 / 30.0.
+constexpr int kAloneKeys = 256;
 
 // Workgroups of a row item of an 8-bit pool: K/V heads, times the parts of at most 16 heads of a larger group.
 int q8_row_units(const ic_pool_cfg& c) { return c.num_kv_heads * ((c.num_heads / c.num_kv_heads + 15) / 16); }
@@ -670,6 +680,7 @@ void plan_sizes(const ic_pool* pool, const ic_batch_desc* d, PlanSizes& ps, Room
   }
   ic_plan_info& in = ps.info;
   double vec_keys = 0;  // of the row items on the vector kernel
+  int64_t n_few_keys = 0, n_some_keys = 0;  // whole row items of up to kAloneKeys keys, of up to twice as many
   for (int s = 0; s < d->num_seqs; ++s) {
     const int c = d->ctx_len[s], n = d->q_len[s];
     in.table_entries += (c + kBlockSize - 1) / kBlockSize;
@@ -686,6 +697,8 @@ void plan_sizes(const ic_pool* pool, const ic_batch_desc* d, PlanSizes& ps, Room
       const int parts = (klen + ps.row_part - 1) / ps.row_part;
       const bool vec = !ps.q8 && (i < rt.n_few || !rt.rest_group);
       in.row_items += parts;
+      if (parts == 1 && klen <= kAloneKeys) ++n_few_keys;
+      if (parts == 1 && klen <= 2 * kAloneKeys) ++n_some_keys;
       if (!rt.few_unit && vec) vec_keys += klen;
       if (vec) ps.vec_items += parts;
       if (parts > 1 && ps.q8 && n > 1) { in.partial_slots += parts * nr; in.merge_rows += nr; }
@@ -703,6 +716,11 @@ void plan_sizes(const ic_pool* pool, const ic_batch_desc* d, PlanSizes& ps, Room
     }
   }
   const int H = pool->cfg.num_heads, D = pool->cfg.head_dim;
+  if (ps.q8) {  // (see kAloneKeys)
+    const int64_t units = q8_row_units(pool->cfg), places = 2 * kExpectedCus;
+    ps.alone_keys = n_some_keys * units > 2 * places ? 2 * kAloneKeys : n_few_keys * units > places ? kAloneKeys : 0;
+    ps.row_long = in.row_items - (int)(ps.alone_keys == 0 ? 0 : ps.alone_keys == kAloneKeys ? n_few_keys : n_some_keys);
+  }
   const int n_vec = ps.vec_items - ps.few_rows;
   const bool short_rows = n_vec > 0 && vec_keys * (4.0 * D) < n_vec * kShortItemBytes;
   ps.row_per_item = short_rows || (t.decode_part_tokens == 0 && ps.row_part < kDefaultRowPart);
@@ -891,6 +909,11 @@ void plan_fill(const ic_batch_desc* d, const PlanSizes& ps, char* img) {
   std::stable_sort(tiles, tiles + ntiles, [&](const TileItem& a, const TileItem& b) { return weight(a) > weight(b); });
   // The same for row items, within the vector kernel's and the group kernel's share: decode contexts differ 16 : 1.
   const auto longer = [](const RowItem& a, const RowItem& b) { return a.k_end - a.k_begin > b.k_end - b.k_begin; };
+  if (ps.q8) {  // items that a wave has alone come last
+    const auto alone = [&ps](const RowItem& a) { return a.slot < 0 && a.k_end <= ps.alone_keys; };
+    std::stable_sort(rows, rows + ps.info.row_items, [&](const RowItem& a, const RowItem& b) { return alone(a) != alone(b) ? alone(b) : longer(a, b); });
+    return;
+  }
   std::stable_sort(rows, rows + few_first, longer);
   std::stable_sort(rows + ps.vec_items, rows + ps.info.row_items, longer);
 }
@@ -1188,6 +1211,7 @@ static int launch_attention(ic_pool* pool, const PlanSizes& ps, float scale, con
   p.block_bytes = (uint32_t)pool->block_bytes;  // 8-bit pools: at most 2 * 4096 * 16 * 257 bytes
   p.row_units = ps.q8 ? q8_row_units(pool->cfg) : 0;
   p.row_subs = p.row_units / pool->cfg.num_kv_heads;
+  p.row_long = ps.row_long;
   p.row_recip = 65536 / (pool->cfg.num_heads / pool->cfg.num_kv_heads) + 1;
   p.q = (const uint16_t*)dev_q;
   p.out = (uint16_t*)dev_out;

@@ -103,6 +103,7 @@ struct AttnParams {
   uint32_t block_bytes;
   int32_t row_units;       // workgroups per row item, K/V heads x row_subs
   int32_t row_subs;        // parts of at most 16 heads of a group
+  int32_t row_long;        // row items [0, row_long) have a workgroup each per unit, the others a wave
   int32_t row_recip;       // c * row_recip >> 16 is c / group for c < 16
 };
 

@@ -223,12 +223,14 @@ __device__ __forceinline__ void finish_row(const AttnParams& p, int slot, int un
 // kMerge: split decode rows are merged by their last partition, else by the merge kernel.
 // kSlim: Q^T stays in LDS behind the rings, which takes 16 registers less.
 // kPair: the item has at most 8 columns; lanes n and n + 8 share one.
-template <int D, int FMT, bool kMerge, bool kSlim, bool kPair>
-__device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* s_last) {
+// kAlone: the wave has an item of its own (whole rows of few keys), no partner, and meets no barrier.
+template <int D, int FMT, bool kMerge, bool kSlim, bool kPair, bool kAlone>
+__device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* s_last, uint32_t item_idx) {
   using R = R8<D>;
-  const uint32_t item_idx = blockIdx.z * kGridItems + blockIdx.y;
+  constexpr int kTeam = kAlone ? 1 : kWaves;                  // waves that share an item
+  constexpr int kRing = kAlone && kSlim ? R::kStages - 1 : R::kStages;  // (Q^T takes the last stage)
   const int unit = (int)blockIdx.x;
-  const RowItem it = p.row_items[p.group_first + item_idx];
+  const RowItem it = p.row_items[item_idx];
   const int n_rows = it.pad[0], pos0 = it.pad[1], nparts = it.pad[2];
   const int H = p.num_heads, Hk = p.num_kv_heads, G = p.group;
   const int subs = p.row_subs;                   // units of a K/V head: more than one where a group has more than 16 heads
@@ -246,7 +248,7 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
 
   bf16x8 q[2 * R::kKL];
   typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
-  lds_bf16x8* const q_lds = (lds_bf16x8*)(lds + kWaves * R::kSlice) + lane;  // operand i of the lane at q_lds[64 i]
+  lds_bf16x8* const q_lds = (lds_bf16x8*)(kAlone ? lds + w * R::kSlice + kRing * (R::kStage / 4) : lds + kWaves * R::kSlice) + lane;  // operand i of the lane at q_lds[64 i]
   {
     const uint16_t* qp = p.q + ((int64_t)(it.qrow + row) * H + head) * D + 16 * g;
 #pragma unroll
@@ -267,7 +269,8 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
   const int last_blk = (it.k_end - 1) / kBlockSize;
   const int n_tiles = (it.k_end - it.k_begin + kKeys - 1) / kKeys;
   const float sc = p.scale_log2e;
-  const int n_mine = (n_tiles - w + kWaves - 1) / kWaves;  // tiles of this wave
+  const int first_tile = kAlone ? 0 : w;
+  const int n_mine = (n_tiles - first_tile + kTeam - 1) / kTeam;  // tiles of this wave
 
   // ---- copies: lane i fills chunk i of every KiB of a stage
   typedef __attribute__((address_space(3))) const char lds_char;
@@ -448,43 +451,44 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
   };
 
   // Q and the first tiles are asked for together; from the wait for Q on, no load but copies is in flight.
-  const int blk0 = it.k_begin / kBlockSize + 2 * w;
-  const auto block = [&](int i, int b) { return bt[min(blk0 + 2 * kWaves * i + b, last_blk)]; };  // of this wave's tile i
-  for (int i = 0; i < R::kStages && i < n_mine; ++i) fetch(yes, yes, block(i, 0), block(i, 1), ring_at + i * R::kStage);
+  const int blk0 = it.k_begin / kBlockSize + 2 * first_tile;
+  const auto block = [&](int i, int b) { return bt[min(blk0 + 2 * kTeam * i + b, last_blk)]; };  // of this wave's tile i
+  for (int i = 0; i < kRing && i < n_mine; ++i) fetch(yes, yes, block(i, 0), block(i, 1), ring_at + i * R::kStage);
   // Ids of the tile that is asked for next, loaded an iteration ahead (waited for where they are used: 8 rows of 1000..8000 keys, 64 heads
   // over 8, plan and 4 layers 102 -> 100 us; 128 rows beside 8 chunks, 40 heads, 582 -> 575).
-  int id0 = block(R::kStages, 0), id1 = block(R::kStages, 1);
+  int id0 = block(kRing, 0), id1 = block(kRing, 1);
 #pragma unroll
   for (int j = 0; j < 2 * R::kKL; ++j) asm volatile("" ::"v"(q[j]));
   if constexpr (kSlim) {
-    if (w == 0)
+    if (kAlone || w == 0)
 #pragma unroll
       for (int i = 0; i < 2 * R::kKL; ++i) q_lds[64 * i] = q[i];
-    __syncthreads();
+    if constexpr (kAlone) asm volatile("" ::: "memory");  // a wave's LDS operations stay in order
+    else __syncthreads();
   }
   if constexpr (R::kStages > 1) {
     uint32_t at = 0;
     for (int i = 0; i < n_mine; ++i) {
       // the copies behind this tile's stay in flight
-      const int behind = min(n_mine - 1 - i, R::kStages - 1);
+      const int behind = min(n_mine - 1 - i, kRing - 1);
       if (behind == 0) wait_copies<0>();
       else if (behind == 1) wait_copies<R::kCopies>();
       else wait_copies<2 * R::kCopies>();
-      step(w + kWaves * i, at, [] {}, [] {});
-      if (i + R::kStages < n_mine) {
+      step(first_tile + kTeam * i, at, [] {}, [] {});
+      if (i + kRing < n_mine) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage has been read
         fetch(yes, yes, id0, id1, ring_at + at);
-        id0 = block(i + 1 + R::kStages, 0);
-        id1 = block(i + 1 + R::kStages, 1);
+        id0 = block(i + 1 + kRing, 0);
+        id1 = block(i + 1 + kRing, 1);
       }
-      at = at + R::kStage == (uint32_t)R::kWaveLds ? 0u : at + R::kStage;
+      at = at + R::kStage == (uint32_t)(kRing * R::kStage) ? 0u : at + R::kStage;
     }
   } else {
     for (int i = 0; i < n_mine; ++i) {
       const bool more = i + 1 < n_mine;
       wait_copies<R::kCopiesV>();  // the values behind the keys stay in flight
       step(
-          w + kWaves * i, 0u,
+          first_tile + kTeam * i, 0u,
           [&]() __attribute__((always_inline)) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             if (more) fetch(yes, no, id0, id1, ring_at);
@@ -500,7 +504,7 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
     }
   }
 
-  // ---- the waves' results meet in LDS: O^T as [column][dim], then (m, l) of every column
+  // ---- the waves' results meet in LDS (alone: change their lanes there): O^T as [column][dim], then (m, l) of every column
   int tid_e = threadIdx.x;
   asm volatile("" : "+v"(tid_e));  // lane numbers worked out again, not kept across the loop
   const int ne = tid_e & 15, ge = (tid_e >> 4) & 3;
@@ -524,22 +528,24 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
       mine[kCols * D + 2 * ne + 1] = l;
     }
   }
-  __syncthreads();
-  for (int idx = tid_e; idx < cols * D; idx += 64 * kWaves) {
+  if constexpr (kAlone) asm volatile("" ::: "memory");
+  else __syncthreads();
+  const float* const all = kAlone ? mine : lds;
+  for (int idx = kAlone ? tid_e & 63 : tid_e; idx < cols * D; idx += 64 * kTeam) {
     const int c = idx / D, d = idx % D;
     float M = kNegBig;
 #pragma unroll
-    for (int ww = 0; ww < kWaves; ++ww) M = __builtin_fmaxf(M, lds[ww * R::kSlice + kCols * D + 2 * c]);
+    for (int ww = 0; ww < kTeam; ++ww) M = __builtin_fmaxf(M, all[ww * R::kSlice + kCols * D + 2 * c]);
     float L = 0.f, O = 0.f;
 #pragma unroll
-    for (int ww = 0; ww < kWaves; ++ww) {
-      const float* sl = lds + ww * R::kSlice;
+    for (int ww = 0; ww < kTeam; ++ww) {
+      const float* sl = all + ww * R::kSlice;
       const float wgt = __builtin_amdgcn_exp2f(sl[kCols * D + 2 * c] - M);
       L = __builtin_fmaf(sl[kCols * D + 2 * c + 1], wgt, L);
       O = __builtin_fmaf(sl[c * D + d], wgt, O);
     }
     const int r = row_of(c), h = head0 + (c - r * heads);
-    if (it.slot < 0) {
+    if (kAlone || it.slot < 0) {
       const __bf16 v = (__bf16)(O / L);  // round to nearest even
       p.out[((int64_t)(it.qrow + r) * H + h) * D + d] = __builtin_bit_cast(uint16_t, v);
     } else {
@@ -551,18 +557,25 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
       }
     }
   }
-  if constexpr (kMerge) {
+  if constexpr (kMerge && !kAlone) {
     if (it.slot >= 0 && nparts == 0) finish_row<D>(p, it.slot, unit, head0, heads, lds, s_last);
   }
 }
 
+// Work items [0, row_long) have a workgroup each, of the others every wave has one.
 template <int D, int FMT, bool kMerge, bool kSlim>
 __device__ __forceinline__ void rows_any(const AttnParams& p, float* lds, int* s_last) {
-  const uint32_t item_idx = blockIdx.z * kGridItems + blockIdx.y;
-  if (item_idx >= (uint32_t)(p.n_row_items - p.group_first)) return;
+  const uint32_t y = blockIdx.z * kGridItems + blockIdx.y, n_items = (uint32_t)p.n_row_items, n_long = (uint32_t)p.row_long;
   const int heads = p.row_subs == 1 ? p.group : kCols;  // (the last part of a larger group may have fewer)
-  if (p.row_items[p.group_first + item_idx].pad[0] * heads <= 8) rows_body<D, FMT, kMerge, kSlim, true>(p, lds, s_last);
-  else rows_body<D, FMT, kMerge, kSlim, false>(p, lds, s_last);
+  if (y < n_long) {
+    if (p.row_items[y].pad[0] * heads <= 8) rows_body<D, FMT, kMerge, kSlim, true, false>(p, lds, s_last, y);
+    else rows_body<D, FMT, kMerge, kSlim, false, false>(p, lds, s_last, y);
+  } else {
+    const uint32_t item = n_long + (y - n_long) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (item >= n_items) return;
+    if (p.row_items[item].pad[0] * heads <= 8) rows_body<D, FMT, kMerge, kSlim, true, true>(p, lds, s_last, item);
+    else rows_body<D, FMT, kMerge, kSlim, false, true>(p, lds, s_last, item);
+  }
 }
 
 template <int D, int FMT, bool kMerge>
@@ -616,11 +629,11 @@ hipError_t launch(const AttnParams& p, dim3 grid, bool slim, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_q8_rows(const AttnParams& p, int head_dim, int dtype, bool slim, hipStream_t st) {
-  if (p.n_row_items <= p.group_first) return hipSuccess;
-  if (p.row_subs < 1 || p.row_subs * kCols < p.group || p.row_units != p.num_kv_heads * p.row_subs || p.row_units > 65535 ||
+  if (p.n_row_items <= 0) return hipSuccess;
+  if (p.row_subs < 1 || p.row_subs * kCols < p.group || p.row_units != p.num_kv_heads * p.row_subs || p.row_units > 65535 || p.group_first != 0 || p.row_long < 0 || p.row_long > p.n_row_items ||
       (dtype != kE4m3 && dtype != kInt8))
     return hipErrorInvalidValue;
-  const uint32_t n = (uint32_t)(p.n_row_items - p.group_first);
+  const uint32_t n = (uint32_t)(p.row_long + (p.n_row_items - p.row_long + kWaves - 1) / kWaves);
   const dim3 g((uint32_t)p.row_units, std::min(n, kGridItems), (n + kGridItems - 1) / kGridItems);
   if (g.z > 65535) return hipErrorInvalidValue;
   const bool e4m3 = dtype == kE4m3;

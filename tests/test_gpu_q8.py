@@ -640,3 +640,27 @@ def test_the_same_call_gives_the_same_bits(fmt):
             for _ in range(6):
                 assert np.array_equal(_run(pool, batch, q), first)
         pool.close()
+
+
+@FMT
+@pytest.mark.parametrize("H,Hkv,D", [(8, 8, 64), (8, 8, 128), (3, 3, 256), (5, 1, 128), (12, 2, 64), (24, 1, 128), (16, 2, 256)])
+@pytest.mark.parametrize("tuning", [dict(), dict(row_launch=3), dict(row_launch=2)])
+def test_short_rows_in_numbers(fmt, H, Hkv, D, tuning):
+    """Rows of few keys, more than there are places for workgroups: a wave each.  Among them long rows, split ones, fresh and short chunks."""
+    rng = np.random.default_rng(H + D)
+    units = Hkv * (-(-(H // Hkv) // 16))
+    n = 1100 // units + 3                                        # (row items of up to 256 and of up to 512 keys)
+    ctx = list(rng.integers(1, 70, n)) + [1, 32, 33, 64, 65, 255, 256, 257, 400, 512, 513, 5000, 90, 300, 64, 70]
+    q_len = [1] * (len(ctx) - 4) + [90, 200, 2, 3]
+    blocks = sum(-(-int(c) // 16) for c in ctx) + 5
+    batch = W.assemble_batch(H, D, 16, blocks, ctx, q_len, rng, num_kv_heads=Hkv)
+    pool_bytes = R.random_pool(batch, Hkv, D, fmt, rng)
+    q = W.randn_bf16((sum(q_len), H, D), rng)
+    pool, _ = _pool(pool_bytes, H, Hkv, D, fmt)
+    pool.set_tuning(**tuning)
+    got = _run(pool, batch, q)
+    want, dev = R.attention(pool_bytes, batch, q, Hkv, fmt)
+    _close(got, want, dev)
+    _close(got[:len(ctx) - 4], want[:len(ctx) - 4], dev[:len(ctx) - 4], weights=ROWS_ONLY)
+    assert np.array_equal(got, _run(pool, batch, q))
+    pool.close()
