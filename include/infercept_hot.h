@@ -226,7 +226,7 @@ typedef struct {
                                  1 = alone one workgroup per work item, 2 = persistent, 3 = persistent, alone too
                                  the slim builds that run beside the tile kernel (in a grouped-query pool of
                                  head_dim 128 with groups of up to 16: the slim group kernel).  8-bit pools have one
-                                 row kernel, one workgroup per work item: row_variant and row_slots have no effect there,
+                                 row kernel, a workgroup or a wave per work item: row_variant and row_slots have no effect there,
                                  row_launch 2 or 3 asks for the pair (head_dim 64, 128), 3 for the slim build alone too */
   int32_t row_slots;          /* resident workgroups of the persistent row kernel (and of the slim group kernel);
                                  0 = one per CU */

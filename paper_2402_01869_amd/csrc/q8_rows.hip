@@ -6,7 +6,7 @@
 // conflicts, 1.02 times the bytes fetched.  Beside the tile kernel, one workgroup a CU, the wait for memory is exposed: 4000 to 5000.
 //
 // One workgroup = one row item (up to 16 columns: consecutive query rows of a sequence x the query heads of a K/V head) x one K/V head,
-// 4 waves, wave w the item's 32-key tiles w, w + 4, ...  HBM-bound: a byte of the cache is read once and meets all columns.
+// 4 waves, wave w the item's 32-key tiles w, w + 4, ...; of items of few keys that are many, each wave has one (row_long).  HBM-bound: a byte of the cache is read once and meets all columns.
 // Every wave copies its tiles from the pool straight into a ring of its own in LDS (no registers, no barrier), one or two tiles ahead, and codes
 // become MFMA operands in registers:
 //   - S^T = K Q^T (16x16x32): a lane's A operand is 8 numbers of one key.  It reads 16 bytes of the key, two operands; which dims
@@ -21,8 +21,8 @@
 //     matrix pipe has the time.  The normaliser is the fp32 sum of the unrounded weights, what is lost is 2^-17 of a weight.
 //     Items of up to 8 columns (kPair: decode rows of groups of up to 8 heads) have their first numbers in columns 0..7 and
 //     the second ones in 8..15: half the products, and one sum across lanes at the end.  Beside the tile kernel: 128 rows and 8
-//     chunks, 40 heads, 573 -> 568 us; alone, int8, 8 rows of 1000..3000 keys, 32 heads of 64, 21.2 -> 20.2 us, 200 of 600..1200, 40
-//     heads of 128, 293 -> 289, of 40..300 81 -> 82.5.
+//     chunks, 40 heads, 573 -> 568 us; by itself, int8, 8 rows of 1000..3000 keys, 32 heads of 64, 21.2 -> 20.2 us, 200 of 600..1200,
+//     40 heads of 128, 293 -> 289.
 // Keys a column does not see: score -inf, weight 0, and 0 for the scale of their value, which may be infinite (NaN vectors); codes
 // behind the item's last key are cleared, they may be anything (0 * NaN).
 #include <algorithm>
@@ -40,7 +40,7 @@ using namespace q8;
 constexpr int kWaves = 4;
 constexpr int kKeys = 32;  // of a wave's tile: two blocks
 constexpr int kCols = 16;
-constexpr uint32_t kGridItems = 32768;  // work items in y, the rest of them in z
+constexpr uint32_t kGridItems = 32768;  // work items (or fours of those that a wave has alone) in y, the rest of them in z
 constexpr float kNegBig = -1.0e30f;
 constexpr float kLazyLog2 = 8.0f;  // slack of the running maximum, in log2 units: below it nothing is rescaled
 
