@@ -137,6 +137,12 @@ __device__ __forceinline__ float across(float x) {
   return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x128, 0xf, 0xf, true));
 }
 
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+// As mergep::store_shared.
+__device__ __forceinline__ void store_two(float* a, float x, float y) {
+  __hip_atomic_store((uint64_t*)a, __builtin_bit_cast(uint64_t, (mergep::f32x2){x, y}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
 // End of a partition of a split decode row: as mergep::finish_split (the workgroup that finds the others' partial results there merges
 // them, in an order that does not depend on who is last), but with all 256 threads.  The row's heads x D values are few for one head, and a
 // thread that reads all partitions of its own waits for memory once per batch of them: here a thread has four values of every
@@ -211,7 +217,6 @@ __device__ __forceinline__ void finish_row(const AttnParams& p, int slot, int un
         }
     }
     if (live && set == 0) {
-      typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
       bf16x4 out;
 #pragma unroll
       for (int i = 0; i < 4; ++i) out[i] = (__bf16)(O[i] / L);  // round to nearest even
@@ -531,30 +536,33 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
   if constexpr (kAlone) asm volatile("" ::: "memory");
   else __syncthreads();
   const float* const all = kAlone ? mine : lds;
-  for (int idx = kAlone ? tid_e & 63 : tid_e; idx < cols * D; idx += 64 * kTeam) {
-    const int c = idx / D, d = idx % D;
+  for (int idx = kAlone ? tid_e & 63 : tid_e; idx < cols * (D / 4); idx += 64 * kTeam) {
+    const int c = idx / (D / 4), d = 4 * (idx % (D / 4));
     float M = kNegBig;
 #pragma unroll
     for (int ww = 0; ww < kTeam; ++ww) M = __builtin_fmaxf(M, all[ww * R::kSlice + kCols * D + 2 * c]);
-    float L = 0.f, O = 0.f;
+    float L = 0.f;
+    f32x4 O = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int ww = 0; ww < kTeam; ++ww) {
       const float* sl = all + ww * R::kSlice;
       const float wgt = __builtin_amdgcn_exp2f(sl[kCols * D + 2 * c] - M);
       L = __builtin_fmaf(sl[kCols * D + 2 * c + 1], wgt, L);
-      O = __builtin_fmaf(sl[c * D + d], wgt, O);
+      const f32x4 x = *(const f32x4*)(sl + c * D + d);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) O[i] = __builtin_fmaf(x[i], wgt, O[i]);
     }
     const int r = row_of(c), h = head0 + (c - r * heads);
     if (kAlone || it.slot < 0) {
-      const __bf16 v = (__bf16)(O / L);  // round to nearest even
-      p.out[((int64_t)(it.qrow + r) * H + h) * D + d] = __builtin_bit_cast(uint16_t, v);
+      bf16x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = (__bf16)(O[i] / L);  // round to nearest even
+      *(bf16x4*)(p.out + ((int64_t)(it.qrow + r) * H + h) * D + d) = v;
     } else {
       const int64_t ps = (int64_t)(it.slot + r * nparts) * H + h;
-      mergep::store_shared(&p.part_o[ps * D + d], O);
-      if (d == 0) {
-        mergep::store_shared(&p.part_ml[ps * 2], M);
-        mergep::store_shared(&p.part_ml[ps * 2 + 1], L);
-      }
+      store_two(&p.part_o[ps * D + d], O[0], O[1]);
+      store_two(&p.part_o[ps * D + d + 2], O[2], O[3]);
+      if (d == 0) store_two(&p.part_ml[ps * 2], M, L);
     }
   }
   if constexpr (kMerge && !kAlone) {
