@@ -306,8 +306,9 @@ double serial_us(const LaunchRates& rate, double tiles, const RowLoad& r, bool f
 }
 
 // Row items of an 8-bit pool that a wave has alone, four to a workgroup: whole ones of up to so many keys, once they are more than the places of a
-// workgroup (two to a CU), and of up to twice as many keys once they are more than twice the places.  A workgroup begins and ends
-// in some 3 us, and on a few keys little else; one that has its place at once is done sooner when its four waves share the keys.
+// workgroup (two to a CU), and of up to twice as many keys once they fill the places of all waves.  A workgroup begins and ends
+// in some 3 us, and on a few keys little else; one that has its place at once is done sooner when its four waves share the keys, and so
+// is the last one (28 rows of 250..500 keys, 40 heads, 23.0 / 24.2).
 // Measured, e4m3, in teams / alone, us: 40 heads, 1 row of 120 keys 4.0 / 5.7, 16 of 250 11.1 / 10.0, 64 of 125..250 29.8 / 24.3, of 250..500 52.2 / 45.1,
 // 256 of 30..60 64.5 / 30.1, of 250..500 173 / 159; 32 heads, 223 of 1..2 40.9 / 14.4; 64 over 8, 256 of 125..250 27.6 / 23.4; 16 of 256 dims, 256 of
 // 60..120 45.9 / 35.3; 8 fresh chunks of 300..800, 64 over 8, whose first 63 rows are such items beside the tiles, 111.6 / 98.2, one of 512, 40 heads (160
@@ -718,7 +719,7 @@ void plan_sizes(const ic_pool* pool, const ic_batch_desc* d, PlanSizes& ps, Room
   const int H = pool->cfg.num_heads, D = pool->cfg.head_dim;
   if (ps.q8) {  // (see kAloneKeys)
     const int64_t units = q8_row_units(pool->cfg), places = 2 * kExpectedCus;
-    ps.alone_keys = n_some_keys * units > 2 * places ? 2 * kAloneKeys : n_few_keys * units > places ? kAloneKeys : 0;
+    ps.alone_keys = n_some_keys * units > 4 * places ? 2 * kAloneKeys : n_few_keys * units > places ? kAloneKeys : 0;
     ps.row_long = in.row_items - (int)(ps.alone_keys == 0 ? 0 : ps.alone_keys == kAloneKeys ? n_few_keys : n_some_keys);
   }
   const int n_vec = ps.vec_items - ps.few_rows;

@@ -644,12 +644,12 @@ def test_the_same_call_gives_the_same_bits(fmt):
 
 @FMT
 @pytest.mark.parametrize("H,Hkv,D", [(8, 8, 64), (8, 8, 128), (3, 3, 256), (5, 1, 128), (12, 2, 64), (24, 1, 128), (16, 2, 256)])
-@pytest.mark.parametrize("tuning", [dict(), dict(row_launch=3), dict(row_launch=2)])
-def test_short_rows_in_numbers(fmt, H, Hkv, D, tuning):
+@pytest.mark.parametrize("tuning,items", [(dict(), 600), (dict(), 2100), (dict(row_launch=3), 2100), (dict(row_launch=2), 600)])
+def test_short_rows_in_numbers(fmt, H, Hkv, D, tuning, items):
     """Rows of few keys, more than there are places for workgroups: a wave each.  Among them long rows, split ones, fresh and short chunks."""
     rng = np.random.default_rng(H + D)
     units = Hkv * (-(-(H // Hkv) // 16))
-    n = 1100 // units + 3                                        # (row items of up to 256 and of up to 512 keys)
+    n = items // units + 3                                       # (600: those of up to 256 keys are a wave's, 2100: of up to 512)
     ctx = list(rng.integers(1, 70, n)) + [1, 32, 33, 64, 65, 255, 256, 257, 400, 512, 513, 5000, 90, 300, 64, 70]
     q_len = [1] * (len(ctx) - 4) + [90, 200, 2, 3]
     blocks = sum(-(-int(c) // 16) for c in ctx) + 5
