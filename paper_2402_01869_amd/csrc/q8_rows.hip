@@ -7,7 +7,7 @@
 //
 // One workgroup = one row item (up to 16 columns: consecutive query rows of a sequence x the query heads of a K/V head) x one K/V head,
 // 4 waves, wave w the item's 32-key tiles w, w + 4, ...; of items of few keys that are many, each wave has one (row_long).  HBM-bound: a byte of the cache is read once and meets all columns.
-// Every wave copies its tiles from the pool straight into a ring of its own in LDS (no registers, no barrier), one or two tiles ahead, and codes
+// Every wave copies its tiles from the pool straight into a ring of its own in LDS (no registers, no barrier), a tile ahead, and codes
 // become MFMA operands in registers:
 //   - S^T = K Q^T (16x16x32): a lane's A operand is 8 numbers of one key.  It reads 16 bytes of the key, two operands; which dims
 //     an operand's 8 places are does not matter as long as Q^T has the same, so Q is loaded in that order.  The accumulator
@@ -55,8 +55,10 @@ struct R8 {
   static constexpr int kCopies = kCopiesK + kCopiesV;
   static constexpr int kStage = 4 * kTile + 512;
   // head_dim 256: one stage, whose keys are copied anew as soon as they are read, then its values.  Two stages (33 KiB a wave) let one
-  // workgroup on a CU, and nothing covers its beginning and end.
-  static constexpr int kStages = D == 64 ? 3 : D == 128 ? 2 : 1;
+  // workgroup on a CU, and nothing covers its beginning and end.  head_dim 64: two stages and four workgroups on a CU; three and two
+  // were slower (256 rows of 500..1000 keys, 32 heads, 147 -> 131 us, of 30..60 18.0 -> 14.1).  head_dim 128: with one stage and four workgroups
+  // rows of 30..60 keys take 10 % less, long ones 2 to 8 % longer.
+  static constexpr int kStages = D == 256 ? 1 : 2;
   static constexpr int kWaveLds = kStages * kStage;
   static constexpr int kSlice = kWaveLds / 4;           // floats of one wave's LDS: at the end its result
   static_assert((kCols * D + 2 * kCols) * 4 <= kWaveLds, "a wave's result takes the place of its ring");
@@ -474,11 +476,9 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
   if constexpr (R::kStages > 1) {
     uint32_t at = 0;
     for (int i = 0; i < n_mine; ++i) {
-      // the copies behind this tile's stay in flight
-      const int behind = min(n_mine - 1 - i, kRing - 1);
-      if (behind == 0) wait_copies<0>();
-      else if (behind == 1) wait_copies<R::kCopies>();
-      else wait_copies<2 * R::kCopies>();
+      // the copies of the tile behind this one stay in flight
+      if (kRing == 1 || i == n_mine - 1) wait_copies<0>();
+      else wait_copies<R::kCopies>();
       step(first_tile + kTeam * i, at, [] {}, [] {});
       if (i + kRing < n_mine) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage has been read
