@@ -73,11 +73,11 @@ typedef struct {
  *
  * A vector x (one token's key, or value, of one head) is head_dim codes and one scale byte b:
  *      a = max |x|,  e = the smallest integer >= -100 with a <= top * 2^e,  b = e + 127
- *      code = x / 2^e rounded to nearest even,  value = code * 2^e
+ *      code = x / 2^e rounded to nearest even (the code below in magnitude where that stands for 2^128),  value = code * 2^e
  *   IC_DTYPE_E4M3  codes are e4m3 numbers (4 bits of significand, no infinities), top = 448
  *   IC_DTYPE_INT8  codes are two's complement integers, top = 127
- * A value is exact in bf16.  It is off from x by at most half a step: 2^-4 of |x| for e4m3 (for |x| >= 2^-6 * 2^e; below, 2^-10 * 2^e),
- * 2^(e-1) for int8, which is less than a / 127 (e > -100).  (A finite a within half a step of the largest bf16 number may round to infinity.)
+ * A value is exact in bf16, and finite.  It is off from x by at most half a step: 2^-4 of |x| for e4m3 (for |x| >= 2^-6 * 2^e; below, 2^-10 * 2^e),
+ * 2^(e-1) for int8, which is less than a / 127 (e > -100); int8 numbers from 63.5 * 2^122 (3.38e38) on by up to 0.75 * 2^122.
  * A vector with a NaN or an infinity in it is kept as b = 255 and codes 0: all its values are NaN.
  *
  * Block of an 8-bit pool: codes [kv][kv_head][slot][dim], one byte each, then scale bytes [kv_head][kv][slot]; the block's size is

@@ -2,7 +2,8 @@
 //
 // A vector x[0..D) (one token's key or value of one head) is D codes and one scale byte b:
 //   a = max |x|,  e = the smallest integer >= -100 with a <= top * 2^e  (top: 448 for e4m3, 127 for int8),
-//   code = x / 2^e rounded to nearest even,  b = e + 127,  value = code * 2^e.
+//   code = x / 2^e rounded to nearest even,  b = e + 127,  value = code * 2^e,
+// and where that value is 2^128 or -2^128, which bf16 does not hold, the code below in magnitude: a finite vector has finite values.
 // A power of two makes x / 2^e and code * 2^e exact: the code's rounding is the only one, and a value (4 or 7 significant bits) is a
 // bf16 number, so a tile that is expanded into LDS, or read back, is the cache's content itself.  One byte a vector (M = 2 Hkv (D + 1)
 // bytes a token); an fp32 scale would use the codes' range better by half a bit in the mean, and cost 3 % more bytes at head_dim 128.

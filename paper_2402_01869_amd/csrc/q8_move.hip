@@ -51,6 +51,18 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t bits) {
   return (uint32_t)max(b, 27);
 }
 
+// The largest numbers under the largest scale round to 2^128, which bf16 does not hold: e4m3, e = 120, from 248 * 2^120 on (codes of 256), integers,
+// e = 122, from 63.5 * 2^122 on (codes of 64).  They are lowered to the bf16 number below those, which rounds to the code below.  (As
+// they came they would be read as infinity, and weight 0 times infinity is NaN: a row that does not see the key would have it too.)
+template <int FMT>
+constexpr uint32_t kLastScale = FMT == kE4m3 ? 247u : 249u;
+template <int FMT>
+__device__ __forceinline__ void keep_finite(u32x4& a) {
+  constexpr uint32_t kMost = FMT == kE4m3 ? 0x7f77u : 0x7f7du;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a[i] = (a[i] & 0x80008000u) | min(a[i] & 0x7fffu, kMost) | min(a[i] >> 16 & 0x7fffu, kMost) << 16;
+}
+
 // Four numbers (two pairs of bf16) as codes; scale = 2^e, inv = 2^-e.
 template <int FMT>
 __device__ __forceinline__ uint32_t four_codes(uint32_t x, uint32_t y, float scale, float inv) {
@@ -115,6 +127,7 @@ __global__ __launch_bounds__(kThreads) void q8_write_kernel(char* __restrict__ p
   for (int u = 0; u < kRows; ++u) {
     const uint32_t sb = scale_byte<FMT>(largest_of_group<(int)Piece<D>::kLanes>(largest_bits(a[u])));
     if (d[u] < 0) continue;
+    if (sb == kLastScale<FMT>) keep_finite<FMT>(a[u]);
     const float scale = __builtin_bit_cast(float, sb << 23), inv = __builtin_bit_cast(float, (254u - sb) << 23);
     u32x2 c = {four_codes<FMT>(a[u][0], a[u][1], scale, inv), four_codes<FMT>(a[u][2], a[u][3], scale, inv)};
     if (sb == 255u) c = (u32x2){0u, 0u};
