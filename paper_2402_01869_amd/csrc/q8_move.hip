@@ -57,10 +57,9 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t bits) {
 template <int FMT>
 constexpr uint32_t kLastScale = FMT == kE4m3 ? 247u : 249u;
 template <int FMT>
-__device__ __forceinline__ void keep_finite(u32x4& a) {
+__device__ __forceinline__ uint32_t kept_finite(uint32_t x) {
   constexpr uint32_t kMost = FMT == kE4m3 ? 0x7f77u : 0x7f7du;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) a[i] = (a[i] & 0x80008000u) | min(a[i] & 0x7fffu, kMost) | min(a[i] >> 16 & 0x7fffu, kMost) << 16;
+  return (x & 0x80008000u) | min(x & 0x7fffu, kMost) | min(x >> 16 & 0x7fffu, kMost) << 16;
 }
 
 // Four numbers (two pairs of bf16) as codes; scale = 2^e, inv = 2^-e.
@@ -127,9 +126,13 @@ __global__ __launch_bounds__(kThreads) void q8_write_kernel(char* __restrict__ p
   for (int u = 0; u < kRows; ++u) {
     const uint32_t sb = scale_byte<FMT>(largest_of_group<(int)Piece<D>::kLanes>(largest_bits(a[u])));
     if (d[u] < 0) continue;
-    if (sb == kLastScale<FMT>) keep_finite<FMT>(a[u]);
+    uint32_t x[4] = {a[u][0], a[u][1], a[u][2], a[u][3]};
+    if (sb == kLastScale<FMT>) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = kept_finite<FMT>(x[i]);
+    }
     const float scale = __builtin_bit_cast(float, sb << 23), inv = __builtin_bit_cast(float, (254u - sb) << 23);
-    u32x2 c = {four_codes<FMT>(a[u][0], a[u][1], scale, inv), four_codes<FMT>(a[u][2], a[u][3], scale, inv)};
+    u32x2 c = {four_codes<FMT>(x[0], x[1], scale, inv), four_codes<FMT>(x[2], x[3], scale, inv)};
     if (sb == 255u) c = (u32x2){0u, 0u};
     const uint32_t blk = (uint32_t)d[u] / (uint32_t)kBlockSize, slot = (uint32_t)d[u] % (uint32_t)kBlockSize;
     char* base = pool + blk * block_bytes;
