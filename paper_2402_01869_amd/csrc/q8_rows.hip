@@ -42,7 +42,10 @@ constexpr int kKeys = 32;  // of a wave's tile: two blocks
 constexpr int kCols = 16;
 constexpr uint32_t kGridItems = 32768;  // work items (or fours of those that a wave has alone) in y, the rest of them in z
 constexpr float kNegBig = -1.0e30f;
-constexpr float kLazyLog2 = 8.0f;  // slack of the running maximum, in log2 units: below it nothing is rescaled
+// Slack of the running maximum, in log2 units: below it nothing is rescaled.  A weight is then at most two to that power, and times the largest
+// scale (2^120, integers 2^122) has to stay finite, in bf16 too: infinity would make NaN of the dimensions whose codes are 0.
+template <int FMT>
+constexpr float kLazyLog2 = FMT == kE4m3 ? 7.0f : 5.0f;
 
 // A wave's ring of stages in LDS: 32 keys as they lie in the cache, K of the two blocks, V of the two blocks, their scale bytes.
 template <int D>
@@ -399,11 +402,11 @@ __device__ __forceinline__ void rows_body(const AttnParams& p, float* lds, int* 
 #pragma unroll
     for (int i = 1; i < 8; ++i) top = __builtin_fmaxf(top, x[i]);
     top *= sc;
-    // the running maximum moves, and the sums with it, only when some score is over it by more than kLazyLog2
-    if (__builtin_amdgcn_ballot_w64(top > m + kLazyLog2) != 0) {
+    // the running maximum moves, and the sums with it, only when some score is over it by more than the slack
+    if (__builtin_amdgcn_ballot_w64(top > m + kLazyLog2<FMT>) != 0) {
       top = __builtin_fmaxf(top, __shfl_xor(top, 16));
       top = __builtin_fmaxf(top, __shfl_xor(top, 32));
-      const float m_new = top > m + kLazyLog2 ? top : m;  // the same in the four lanes of a column
+      const float m_new = top > m + kLazyLog2<FMT> ? top : m;  // the same in the four lanes of a column
       const float was = __builtin_amdgcn_exp2f(m - m_new);
       m = m_new;
       l *= was;

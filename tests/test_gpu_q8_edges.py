@@ -141,3 +141,45 @@ def test_the_largest_number_in_a_key_meets_zeros(fmt, H, Hkv, D, tuning):
     assert np.isfinite(got).all()
     assert (np.abs(got - want) <= (2.0 ** -8 + 1e-5) * np.abs(want) + (2.0 ** -8 + 1e-3) * dev + 1e-6).all()
     pool.close()
+
+
+@FMT
+@pytest.mark.parametrize("H,Hkv,D", [(2, 2, 64), (2, 2, 128), (16, 1, 128), (1, 1, 256)])
+@pytest.mark.parametrize("tuning", [dict(), dict(decode_part_tokens=192), dict(row_launch=3)])
+def test_a_weight_ahead_of_the_running_maximum_meets_the_largest_scale(fmt, H, Hkv, D, tuning):
+    """A key that scores 2^7.9 times the ones before it, by less than the running maximum's slack may be: its weight times the scale of a value
+    with the largest bf16 number stays finite, and the dimensions where that value is 0 are the 64-bit result."""
+    ctx = [150, 300, 170, 190]
+    q_len = [1, 1, 3, 1]
+    rng = np.random.default_rng(3)
+    batch = W.assemble_batch(H, D, 16, 60, ctx, q_len, rng, num_kv_heads=Hkv)
+    batch.scale = 1.0
+    whole = W.Batch(H, D, 16, 60, batch.ctx_len, batch.ctx_len, np.cumsum([0] + ctx[:-1]).astype(np.int32), batch.block_tables, 1.0, num_kv_heads=Hkv)
+    k, v = np.zeros((sum(ctx), Hkv, D), np.uint16), W.randn_bf16((sum(ctx), Hkv, D), rng)
+    for s, c in enumerate(ctx):
+        r = int(whole.q_start[s]) + 133                          # the fifth tile of 32 keys: the first wave has the first tile and this one
+        k[r, :, 0] = W.f32_to_bf16_bits(np.float32(5.5))         # 7.93 in powers of two
+        v[r] &= 0x8000
+        v[r, :, 7] = LARGEST
+    q = W.randn_bf16((sum(q_len), H, D), rng)
+    q[:, :, 0] = W.f32_to_bf16_bits(np.float32(1.0))
+    start = R.empty_pool(60, Hkv, D)
+    host = start.copy()
+    _write(host, whole, k, v, fmt)
+    t = torch.from_numpy(start).to(DEV)
+    pool = B.KvPool.from_tensor(t, H, D, num_kv_heads=Hkv, dtype=R.FORMATS[fmt])
+    kt, vt, qt, out = to_dev_bits(k), to_dev_bits(v), to_dev_bits(q), torch.zeros(q.shape, dtype=torch.int16, device=DEV)
+    pool.kv_write_span(B.HostDesc.from_batch(whole), kt.data_ptr(), vt.data_ptr())
+    pool.set_tuning(**tuning)
+    desc = B.HostDesc.from_batch(batch)
+    ws = torch.empty(pool.workspace_bytes(desc), dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    pool.paged_attn_mixed(desc, qt.data_ptr(), out.data_ptr(), ws.data_ptr(), ws.numel())
+    torch.cuda.synchronize()
+    got = W.bf16_bits_to_f64(from_dev_bits(out))
+    want, dev = R.attention(host, batch, q, Hkv, fmt)
+    others = np.arange(D) != 7
+    got, want, dev = got[..., others], want[..., others], dev[..., others]
+    assert np.isfinite(got).all()
+    assert (np.abs(got - want) <= (2.0 ** -8 + 1e-5) * np.abs(want) + 1e-3 * dev + 1e-6).all()
+    pool.close()
