@@ -304,7 +304,8 @@ typedef struct {
   int32_t n_few_items, n_few_rows;
   int32_t n_merged_inside;  /* merge items [0, n) are merged by the row or group kernel, the rest by the merge kernel */
   int32_t n_split_slots;    /* entries of slot_merge                                                  */
-  int32_t n_split_units;    /* units of such a row: query heads, or K/V heads on the group kernel     */
+  int32_t n_split_units;    /* units of such a row: query heads, or K/V heads on the group kernel (8-bit pools: times the
+                               parts of at most 16 heads of a larger group)                            */
   int32_t reserved;
 } ic_plan_launch_info;
 int ic_plan_launches(const ic_pool* pool, const ic_batch_desc* desc, ic_plan_launch_info* out);

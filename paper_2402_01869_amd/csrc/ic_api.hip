@@ -572,8 +572,9 @@ int choose_span_part(const ic_pool* pool, const ic_batch_desc* d, const PlanSize
 // of 600..10200 keys, 40 heads, in 4096-key items 729 us a layer against 710 with the merge kernel.
 int split_units(const ic_pool* pool, const PlanSizes& ps) {
   const ic_tuning& t = pool->tune;
-  if (t.decode_part_tokens > 0 || t.row_launch > 1 || t.row_slots > 0 || ps.row_part >= kDefaultRowPart || ps.side_by_side) return 0;
-  if (ps.q8) return q8_row_units(pool->cfg);
+  if (t.decode_part_tokens > 0 || ps.row_part >= kDefaultRowPart || ps.side_by_side) return 0;
+  if (ps.q8) return t.row_launch == 3 && pool->cfg.head_dim <= 128 ? 0 : q8_row_units(pool->cfg);  // (all but the slim build merge)
+  if (t.row_launch > 1 || t.row_slots > 0) return 0;
   return ps.decode_as_group ? pool->cfg.num_kv_heads : pool->cfg.num_heads;
 }
 

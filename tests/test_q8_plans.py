@@ -1,0 +1,52 @@
+"""Launch plans of 8-bit pools without a GPU: what the tuning's fields change, and what the pool's size may be."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+import q8_ref as R
+from paper_2402_01869_amd import binding as B
+from paper_2402_01869_amd import workloads as W
+
+FMT = pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+
+
+def _pool(fmt, blocks, H, D, Hkv=None):
+    return B.KvPool(B.make_cfg(blocks, H, D, num_kv_heads=Hkv, dtype=R.FORMATS[fmt]), 0x1000000, blocks * B.block_bytes(Hkv or H, D, 16, R.FORMATS[fmt]))
+
+
+def _image(pool, desc):
+    """The bytes of the descriptor image, and what would be launched."""
+    lay, how = B.PlanLayout(), B.PlanLaunchInfo()
+    assert B.lib().ic_plan_image(pool._h, C.byref(desc.struct), None, 0, C.byref(lay)) == B.IC_OK
+    img = np.zeros(lay.image_bytes, dtype=np.uint8)
+    assert B.lib().ic_plan_image(pool._h, C.byref(desc.struct), img.ctypes.data_as(C.c_void_p), img.nbytes, C.byref(lay)) == B.IC_OK
+    assert B.lib().ic_plan_launches(pool._h, C.byref(desc.struct), C.byref(how)) == B.IC_OK
+    return img.tobytes(), bytes(lay), bytes(how), pool.workspace_bytes(desc)
+
+
+@FMT
+@pytest.mark.parametrize("H,Hkv,D", [(8, 8, 128), (16, 2, 64), (24, 1, 128), (4, 4, 256)])
+@pytest.mark.parametrize("tuning", [dict(row_slots=128), dict(row_slots=65536), dict(row_variant=3), dict(row_slots=64, row_variant=1)])
+@pytest.mark.parametrize("ctx,q_len", [([3000], [1]), ([3000, 90, 700], [1, 1, 1]), ([2500, 3000, 400], [1, 300, 3])])
+def test_fields_of_the_vector_row_kernel_have_no_effect(fmt, H, Hkv, D, tuning, ctx, q_len):
+    batch = W.assemble_batch(H, D, 16, 500, ctx, q_len, np.random.default_rng(1), num_kv_heads=Hkv)
+    pool, desc = _pool(fmt, 500, H, D, Hkv), B.HostDesc.from_batch(batch)
+    plain = _image(pool, desc)
+    pool.set_tuning(**tuning)
+    assert _image(pool, desc) == plain
+    pool.close()
+
+
+@FMT
+@pytest.mark.parametrize("H,Hkv,D,ctx,q_len", [(8, 8, 128, [3000, 500], [1, 1]), (16, 2, 64, [3000], [1]), (4, 4, 256, [3000, 500], [1, 1]),
+                                               (4, 4, 256, [3000, 400], [1, 300])])
+def test_asking_for_a_pair_that_there_is_none_of_changes_nothing(fmt, H, Hkv, D, ctx, q_len):
+    """row_launch = 2: no tiles to run beside, or head_dim 256."""
+    batch = W.assemble_batch(H, D, 16, 500, ctx, q_len, np.random.default_rng(1), num_kv_heads=Hkv)
+    pool, desc = _pool(fmt, 500, H, D, Hkv), B.HostDesc.from_batch(batch)
+    plain = _image(pool, desc)
+    for row_launch in (1, 2) + ((3,) if D == 256 else ()):
+        pool.set_tuning(row_launch=row_launch)
+        assert _image(pool, desc) == plain
+    pool.close()
