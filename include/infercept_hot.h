@@ -56,7 +56,7 @@ const char* ic_strerror(int code);
  *   so attention reads it with full-width coalesced loads.
  * ------------------------------------------------------------------------------------------ */
 typedef struct {
-  int32_t num_blocks;   /* >= 1                                                          */
+  int32_t num_blocks;   /* >= 1; 8-bit dtypes: at most 2^27                              */
   int32_t block_size;   /* tokens per block; 16 is the only size built                   */
   int32_t num_heads;    /* query heads                                                   */
   int32_t num_kv_heads; /* K/V heads in the pool; divides num_heads.  Equal: multi-head attention;

@@ -97,6 +97,9 @@ int check_cfg(const ic_pool_cfg* c) {
   if (c->num_kv_heads > c->num_heads || c->num_heads % c->num_kv_heads != 0) return IC_EINVAL;
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return IC_EUNSUPPORTED;
   if (c->num_heads > 4096) return IC_EINVAL;
+  // Cache slots are int32 (block * 16 + slot).  Of the 8-bit pools' smallest block, 2176 bytes, 2^27 are 272 GiB, less than the card has; of a
+  // bf16 pool's, 4 KiB, they are 512.
+  if (c->dtype != IC_DTYPE_BF16 && c->num_blocks > (1 << 27)) return IC_EINVAL;
   return IC_OK;
 }
 

@@ -50,3 +50,20 @@ def test_asking_for_a_pair_that_there_is_none_of_changes_nothing(fmt, H, Hkv, D,
         pool.set_tuning(row_launch=row_launch)
         assert _image(pool, desc) == plain
     pool.close()
+
+
+@FMT
+def test_cache_slots_fit_32_bits(fmt):
+    """Slots are block * 16 + slot in an int32: the last one of 2^27 blocks is 2^31 - 1; a block more would be written nowhere."""
+    H, D, most = 1, 64, 1 << 27
+    bb = B.block_bytes(H, D, 16, R.FORMATS[fmt])
+    p = B.KvPool(B.make_cfg(most, H, D, dtype=R.FORMATS[fmt]), 0x1000000, most * bb)
+    desc = B.HostDesc([16], [16], [0], np.array([[most - 1]], np.int32), 1.0, 16)
+    dst = p.plan_image(desc)["row_dst"]
+    assert dst[0] == (most - 1) * 16 and dst[15] == 2 ** 31 - 1
+    p.close()
+    with pytest.raises(B.InferceptError) as e:
+        B.KvPool(B.make_cfg(most + 1, H, D, dtype=R.FORMATS[fmt]), 0x1000000, (most + 1) * bb)
+    assert e.value.code == B.IC_EINVAL
+    cfg = B.make_cfg(most + 1, H, D, dtype=R.FORMATS[fmt])
+    assert B.lib().ic_check_batch(C.byref(cfg), C.byref(desc.struct)) == B.IC_EINVAL
