@@ -314,7 +314,7 @@ int ic_plan_launches(const ic_pool* pool, const ic_batch_desc* desc, ic_plan_lau
  * Swap of scattered blocks (Section 3.2, swap-based approach: a paged context is scattered over
  * many discontinuous regions, and moving it with one launch per region is launch-bound;
  * Section 4.1 moves it layer by layer, a bounded number of tokens per iteration).  One call moves
- * one layer's K+V of the listed blocks in ONE launch; a chunk of the swap is a shorter id list.
+ * one layer's K+V of the listed blocks in ONE launch (per 64 GiB); a chunk of the swap is a shorter id list.
  *
  *   kv_pack_blocks:    staging[i] <- pool[host_ids[i]]   i < n   (list order; duplicates allowed)
  *   kv_unpack_blocks:  pool[host_ids[i]] <- staging[i]   i < n   (ids must be distinct: IC_EDUP)

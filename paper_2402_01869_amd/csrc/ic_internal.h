@@ -20,6 +20,8 @@ struct PoolView {
 PoolView pool_view(const ic_pool* pool);
 
 constexpr int kBlockSize = 16;  // tokens per cache block (the only size built)
+// Threads of a launch in one grid dimension: fewer than 2^32.  Of a larger grid the runtime starts the remainder, without an error.
+constexpr uint64_t kMaxLaunchThreads = 0xffffffffull;
 constexpr int kRowWaves = 4;    // waves per workgroup of the row kernel
 constexpr int kMaxRowPart = 4096;  // keys per row-kernel work item: 64 block ids per wave
 

@@ -4,6 +4,7 @@
 //
 // Pure byte movement, HBM-bound.  Every lane moves 16 bytes with non-temporal loads and stores;
 // the grid is (blocks in the list) x (chunks per block), hundreds of thousands of workgroups.
+#include <algorithm>
 #include <cstring>
 #include <mutex>
 
@@ -71,12 +72,18 @@ template <bool PACK>
 hipError_t launch_swap(char* pool, char* staging, const int32_t* dev_ids, int32_t n,
                        size_t block_bytes, hipStream_t st) {
   if (n <= 0) return hipSuccess;
+  if (block_bytes > 0xffffffffull) return hipErrorInvalidValue;
   const uint32_t chunks = (uint32_t)((block_bytes + kChunk - 1) / kChunk);
-  const uint64_t grid = (uint64_t)n * chunks;
-  if (grid > 0x7fffffffull || block_bytes > 0xffffffffull) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(swap_blocks_kernel<PACK>, dim3((uint32_t)grid), dim3(kThreads), 0, st, pool,
-                     staging, dev_ids, (uint32_t)block_bytes, chunks, (uint32_t)n);
-  return hipGetLastError();
+  const uint64_t most = kMaxLaunchThreads / kThreads / chunks / 8 * 8;  // blocks of a launch (64 GiB), in the groups of 8 of the kernel
+  if (most == 0) return hipErrorInvalidValue;
+  for (uint64_t i = 0; i < (uint64_t)n; i += most) {
+    const uint32_t count = (uint32_t)std::min<uint64_t>(most, (uint64_t)n - i);
+    hipLaunchKernelGGL(swap_blocks_kernel<PACK>, dim3(count * chunks), dim3(kThreads), 0, st, pool, staging + i * block_bytes, dev_ids + i,
+                       (uint32_t)block_bytes, chunks, count);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // Descriptor upload: pinned host memory -> device, 16 bytes per lane, read over the host link by
@@ -120,17 +127,22 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(char* __restrict__ 
 hipError_t launch_append(void* pool, const void* k_new, const void* v_new, const int32_t* dev_dst, int32_t rows,
                          int num_heads, int head_dim, hipStream_t st) {
   if (rows <= 0) return hipSuccess;
-  const uint64_t lanes = (uint64_t)rows * 2u * (uint64_t)num_heads * (uint64_t)(head_dim / 8);
-  const uint64_t grid = (lanes + kThreads - 1) / kThreads;  // one-wave workgroups, as for the block moves
-  if (grid > 0x7fffffffull) return hipErrorInvalidValue;
-  const dim3 g((uint32_t)grid), b(kThreads);
-  switch (head_dim) {
-    case 64: hipLaunchKernelGGL(kv_append_kernel<64>, g, b, 0, st, (char*)pool, (const char*)k_new, (const char*)v_new, dev_dst, (uint32_t)rows, (uint32_t)num_heads); break;
-    case 128: hipLaunchKernelGGL(kv_append_kernel<128>, g, b, 0, st, (char*)pool, (const char*)k_new, (const char*)v_new, dev_dst, (uint32_t)rows, (uint32_t)num_heads); break;
-    case 256: hipLaunchKernelGGL(kv_append_kernel<256>, g, b, 0, st, (char*)pool, (const char*)k_new, (const char*)v_new, dev_dst, (uint32_t)rows, (uint32_t)num_heads); break;
-    default: return hipErrorInvalidValue;
+  const uint64_t lanes = 2u * (uint64_t)num_heads * (uint64_t)(head_dim / 8);  // of a row
+  const uint64_t most = kMaxLaunchThreads / lanes - 1, row_bytes = lanes * 8;   // rows of a launch (64 GiB); -1: whole workgroups
+  for (uint64_t r = 0; r < (uint64_t)rows; r += most) {
+    const uint32_t n = (uint32_t)std::min<uint64_t>(most, (uint64_t)rows - r);
+    const dim3 g((uint32_t)((n * lanes + kThreads - 1) / kThreads)), b(kThreads);  // one-wave workgroups, as for the block moves
+    const char *k = (const char*)k_new + r * row_bytes, *v = (const char*)v_new + r * row_bytes;
+    switch (head_dim) {
+      case 64: hipLaunchKernelGGL(kv_append_kernel<64>, g, b, 0, st, (char*)pool, k, v, dev_dst + r, n, (uint32_t)num_heads); break;
+      case 128: hipLaunchKernelGGL(kv_append_kernel<128>, g, b, 0, st, (char*)pool, k, v, dev_dst + r, n, (uint32_t)num_heads); break;
+      case 256: hipLaunchKernelGGL(kv_append_kernel<256>, g, b, 0, st, (char*)pool, k, v, dev_dst + r, n, (uint32_t)num_heads); break;
+      default: return hipErrorInvalidValue;
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 hipError_t launch_upload(void* dev_dst, const void* pinned_src, size_t bytes, hipStream_t st) {

@@ -7,6 +7,8 @@
 // some 3.2 a ns, which at 1.5 KiB each (one row) is 4.9 TB/s.  Measured, e4m3, 40 heads of 128: 17143 rows read back 109 us with
 // one row a lane, 102 with two, 95 with four (5.6 TB/s), 98 with eight; 16 numbers a lane and one row, 98; 8320 rows (256 MB)
 // written 42 -> 41 us, read back 42 -> 41 (16 numbers a lane: 57).
+#include <algorithm>
+
 #include "q8.h"
 
 namespace ic {
@@ -195,20 +197,25 @@ __global__ __launch_bounds__(kThreads) void kv_gather_kernel(const char* __restr
 }
 
 template <int D>
-hipError_t move_rows(void* pool, size_t block_bytes, int dtype, bool write, void* k, void* v, const int32_t* dev_rows, int32_t rows, int heads,
+hipError_t move_rows(void* pool, size_t block_bytes, int dtype, bool write, void* k_rows, void* v_rows, const int32_t* dev_rows, int32_t rows, int heads,
                      hipStream_t st) {
-  // 8 numbers a lane, of one row (bf16 pools) or of kRows (8-bit pools)
-  const uint64_t sets = dtype == IC_DTYPE_BF16 ? (uint64_t)rows : ((uint64_t)rows + kRows - 1) / kRows;
-  const uint64_t grid = (sets * 2u * (uint64_t)heads * (uint64_t)(D / 8) + kThreads - 1) / kThreads;
-  if (grid > 0x7fffffffull) return hipErrorInvalidValue;
-  const dim3 g((uint32_t)grid), b(kThreads);
-  const uint32_t n = (uint32_t)rows, h = (uint32_t)heads;
-  if (dtype == IC_DTYPE_BF16) hipLaunchKernelGGL(kv_gather_kernel<D>, g, b, 0, st, (const char*)pool, (char*)k, (char*)v, dev_rows, n, h);
-  else if (dtype == kE4m3 && write) hipLaunchKernelGGL((q8_write_kernel<D, kE4m3>), g, b, 0, st, (char*)pool, block_bytes, (const char*)k, (const char*)v, dev_rows, n, h);
-  else if (dtype == kE4m3) hipLaunchKernelGGL((q8_read_kernel<D, kE4m3>), g, b, 0, st, (const char*)pool, block_bytes, (char*)k, (char*)v, dev_rows, n, h);
-  else if (write) hipLaunchKernelGGL((q8_write_kernel<D, kInt8>), g, b, 0, st, (char*)pool, block_bytes, (const char*)k, (const char*)v, dev_rows, n, h);
-  else hipLaunchKernelGGL((q8_read_kernel<D, kInt8>), g, b, 0, st, (const char*)pool, block_bytes, (char*)k, (char*)v, dev_rows, n, h);
-  return hipGetLastError();
+  // 8 numbers a lane, of one row (bf16 pools) or of a set of kRows (8-bit pools)
+  const uint64_t set = dtype == IC_DTYPE_BF16 ? 1 : kRows, lanes = 2u * (uint64_t)heads * (uint64_t)(D / 8);
+  const uint64_t most = (kMaxLaunchThreads / lanes - 1) * set;  // rows of a launch; -1: whole workgroups
+  for (uint64_t r = 0; r < (uint64_t)rows; r += most) {
+    const uint32_t n = (uint32_t)std::min<uint64_t>(most, (uint64_t)rows - r), h = (uint32_t)heads;
+    const dim3 g((uint32_t)(((n + set - 1) / set * lanes + kThreads - 1) / kThreads)), b(kThreads);
+    char *k = (char*)k_rows + r * lanes * 8, *v = (char*)v_rows + r * lanes * 8;
+    const int32_t* at = dev_rows + r;
+    if (dtype == IC_DTYPE_BF16) hipLaunchKernelGGL(kv_gather_kernel<D>, g, b, 0, st, (const char*)pool, k, v, at, n, h);
+    else if (dtype == kE4m3 && write) hipLaunchKernelGGL((q8_write_kernel<D, kE4m3>), g, b, 0, st, (char*)pool, block_bytes, k, v, at, n, h);
+    else if (dtype == kE4m3) hipLaunchKernelGGL((q8_read_kernel<D, kE4m3>), g, b, 0, st, (const char*)pool, block_bytes, k, v, at, n, h);
+    else if (write) hipLaunchKernelGGL((q8_write_kernel<D, kInt8>), g, b, 0, st, (char*)pool, block_bytes, k, v, at, n, h);
+    else hipLaunchKernelGGL((q8_read_kernel<D, kInt8>), g, b, 0, st, (const char*)pool, block_bytes, k, v, at, n, h);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t move_any(void* pool, size_t block_bytes, int dtype, bool write, void* k, void* v, const int32_t* dev_rows, int32_t rows, int heads,
