@@ -150,6 +150,7 @@ size_t paged_attn_mixed_workspace_bytes(const ic_pool* pool, const ic_batch_desc
  * paged_attn_mixed_workspace_bytes(), or enough to run the batch without the splits that only save time
  * (IC_ESIZE otherwise); its contents are scratch.
  * Deterministic: the same inputs and workspace size give the same bits on every call.
+ * IC_EINVAL also for a batch whose short rows (times heads) are more workgroups than a launch may have: 2^24.
  */
 int paged_attn_mixed(ic_pool* pool, const ic_batch_desc* desc, const void* dev_q, void* dev_out,
                      void* dev_workspace, size_t workspace_bytes, void* hip_stream);

@@ -58,7 +58,7 @@ int ic_mfma_ceiling(const void* dev_operands, size_t operand_bytes, void* dev_si
  * (1 KiB each for the copy, 8 KiB for the read), non-temporal loads and stores.  *gbps = bytes moved
  * (read, or read + written) per second over `reps` back-to-back launches, by HIP events on
  * hip_stream.  Synchronous.
- *   bytes: a multiple of 8192, at most 2^31 KiB; reps 1 .. 10000; the two ranges must not overlap.
+ *   bytes: a multiple of 8192, less than 64 GiB for the copy and 512 GiB for the read; reps 1 .. 10000; the two ranges must not overlap.
  * Errors: IC_ENULL, IC_EINVAL, IC_EALIGN, IC_EHIP; nothing is launched on a validation error.
  */
 int ic_hbm_ceiling(const void* dev_src, void* dev_dst, size_t bytes, int32_t mode, int32_t reps,

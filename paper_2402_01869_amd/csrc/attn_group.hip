@@ -22,7 +22,6 @@ namespace {
 
 using namespace tilep;
 
-constexpr int kGroupWaves = 4;
 constexpr int kGT = 32;  // keys per wave tile: two cache blocks
 
 template <int D>
@@ -269,7 +268,7 @@ hipError_t launch_group_kernel(const AttnParams& p, int head_dim, hipStream_t st
   if (n_items <= 0) return hipSuccess;
   if (p.group < 2 || p.group > 32) return hipErrorInvalidValue;
   const uint64_t grid = (uint64_t)n_items * (uint64_t)p.num_kv_heads;
-  if (grid > 0x7fffffffull) return hipErrorInvalidValue;
+  if (grid * 64 * kGroupWaves > kMaxLaunchThreads) return hipErrorInvalidValue;
   const dim3 g((uint32_t)grid), b(64 * kGroupWaves);
 #define IC_GROUP_CASE(DD)                                                                                  \
   case DD:                                                                                                 \

@@ -48,7 +48,6 @@ __global__ __launch_bounds__(kRowWaves * 64) void row_persist_kernel(AttnParams 
 // consecutive values of one row, 16 bytes per thread and load.  Bound by memory.  Measured against one workgroup of D
 // threads per (row, head), which read 4 bytes per thread and needed the maximum before the first value: 8 rows of 64
 // heads in 2 to 11 partitions 7.3 -> 5.7 us.
-constexpr int kMergeThreads = 256, kMergeElems = 4 * kMergeThreads;
 
 template <int D>
 __global__ __launch_bounds__(kMergeThreads) void merge_kernel(AttnParams p, uint32_t chunks) {
@@ -64,7 +63,7 @@ __global__ __launch_bounds__(kMergeThreads) void merge_kernel(AttnParams p, uint
 hipError_t launch_row_kernel(const AttnParams& p, int head_dim, hipStream_t st) {
   if (p.n_vec_items <= 0) return hipSuccess;
   const uint64_t grid = (uint64_t)p.n_vec_items * p.num_heads;
-  if (grid > 0x7fffffffull) return hipErrorInvalidValue;
+  if (grid * kRowWaves * 64 > kMaxLaunchThreads) return hipErrorInvalidValue;
   const dim3 g((uint32_t)grid), b(kRowWaves * 64);
 #define IC_ROW_CASE(DD)                                                                       \
   case DD:                                                                                    \
@@ -137,7 +136,7 @@ hipError_t launch_merge_kernel(const AttnParams& p, int head_dim, hipStream_t st
   if (p.n_merge_items <= 0) return hipSuccess;
   const uint32_t chunks = ((uint32_t)(p.num_heads * head_dim) + kMergeElems - 1) / kMergeElems;
   const uint64_t grid = (uint64_t)p.n_merge_items * chunks;
-  if (grid > 0x7fffffffull) return hipErrorInvalidValue;
+  if (grid * kMergeThreads > kMaxLaunchThreads) return hipErrorInvalidValue;
   const dim3 g((uint32_t)grid), b(kMergeThreads);
   switch (head_dim) {
     case 64: hipLaunchKernelGGL(merge_kernel<64>, g, b, 0, st, p, chunks); break;

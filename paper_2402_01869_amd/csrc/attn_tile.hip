@@ -126,7 +126,8 @@ hipError_t launch_tile_kernel(const AttnParams& p, int head_dim, hipStream_t st)
   if (head_dim != tile16::kDim) return hipErrorInvalidValue;
   const uint64_t grid = (uint64_t)p.n_tile_items * (uint64_t)(p.num_heads >> p.tile_g_shift) + few_units(p);
   if (grid == 0) return hipSuccess;
-  if (grid > 0x7fffffffull) return hipErrorInvalidValue;
+  static_assert(Impl<tile16::kDim>::kThreads == 512, "the planner counts the threads of a launch");
+  if (grid * Impl<tile16::kDim>::kThreads > kMaxLaunchThreads) return hipErrorInvalidValue;
   hipLaunchKernelGGL(tile_attn_kernel<tile16::kDim>, dim3((uint32_t)grid), dim3(Impl<tile16::kDim>::kThreads), 0, st, p);
   return hipGetLastError();
 }

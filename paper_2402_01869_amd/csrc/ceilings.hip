@@ -92,7 +92,7 @@ extern "C" int ic_paged_read_ceiling(const ic_pool* pool, const int32_t* host_id
   using namespace ic;
   if (!pool || !host_ids || !dev_sink || !gbps) return IC_ENULL;
   const PoolView pv = pool_view(pool);
-  if (n < 1 || reps < 1 || reps > 10000 || (uint64_t)n * (uint64_t)pv.cfg.num_kv_heads > 0x7fffffffull) return IC_EINVAL;
+  if (n < 1 || reps < 1 || reps > 10000 || (uint64_t)n * (uint64_t)pv.cfg.num_kv_heads * 64 > kMaxLaunchThreads) return IC_EINVAL;
   if (pv.cfg.dtype != IC_DTYPE_BF16) return IC_EUNSUPPORTED;  // the probe reads bf16 tiles
   const int rc0 = ic_check_ids(&pv.cfg, host_ids, n, 0);
   if (rc0 != IC_OK) return rc0;
@@ -133,7 +133,7 @@ extern "C" int ic_hbm_ceiling(const void* dev_src, void* dev_dst, size_t bytes, 
   using namespace ic;
   if (!dev_src || !dev_dst || !gbps) return IC_ENULL;
   if ((mode != 0 && mode != 1) || reps < 1 || reps > 10000 || bytes < 8192 || bytes % 8192 != 0 ||
-      bytes / 1024 > 0x7fffffffull)
+      bytes / (mode == 1 ? 1024 : 1024 * kReadChunks) * 64 > kMaxLaunchThreads)
     return IC_EINVAL;
   if (((uintptr_t)dev_src | (uintptr_t)dev_dst) & 15) return IC_EALIGN;
   {

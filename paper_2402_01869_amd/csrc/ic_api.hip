@@ -1200,6 +1200,17 @@ static int upload_plan(ic_pool* pool, const ic_batch_desc* desc, const PlanSizes
   return launch_upload(ws, host, ps.image_bytes, st) == hipSuccess ? IC_OK : IC_EHIP;
 }
 
+// The launches with a workgroup per work item stay within kMaxLaunchThreads.
+static bool launches_fit(const ic_pool* pool, const PlanSizes& ps) {
+  const PlanLaunches how = plan_launches(pool, ps);
+  const uint64_t H = (uint64_t)pool->cfg.num_heads, Hk = (uint64_t)pool->cfg.num_kv_heads, D = (uint64_t)pool->cfg.head_dim;
+  const auto fits = [](uint64_t groups, uint64_t threads) { return groups * threads <= kMaxLaunchThreads; };
+  if (how.row == IC_LAUNCH_PER_ITEM && !fits((uint64_t)(ps.vec_items - ps.few_rows) * H, 64 * kRowWaves)) return false;
+  if (!ps.q8 && how.group == IC_LAUNCH_PER_ITEM && !fits((uint64_t)(ps.info.row_items - ps.vec_items) * Hk, 64 * kGroupWaves)) return false;
+  if (how.tile == IC_LAUNCH_PER_ITEM && !fits((uint64_t)ps.info.tile_items * (H >> ps.tile_g_shift) + (uint64_t)ps.few_runs * ((H + 1) / 2), 512)) return false;
+  return fits((uint64_t)ps.info.merge_rows * ((H * D + kMergeElems - 1) / kMergeElems), kMergeThreads);
+}
+
 // The kernels of one attention call, for a descriptor image that is already in the workspace.
 static int launch_attention(ic_pool* pool, const PlanSizes& ps, float scale, const void* dev_q, void* dev_out,
                             char* ws, hipStream_t st) {
@@ -1353,6 +1364,7 @@ int paged_attn_mixed(ic_pool* pool, const ic_batch_desc* desc, const void* dev_q
     if (misaligned(dev_q) || misaligned(dev_out) || ((uintptr_t)dev_workspace & 255u)) return IC_EALIGN;
     PlanSizes ps;
     if ((rc = plan_within(pool, desc, workspace_bytes, ps)) != IC_OK) return rc;
+    if (!launches_fit(pool, ps)) return IC_EINVAL;
     hipStream_t st = (hipStream_t)hip_stream;
     char* ws = (char*)dev_workspace;
     if ((rc = upload_plan(pool, desc, ps, ws, st)) != IC_OK) return rc;
@@ -1369,6 +1381,7 @@ int paged_attn_plan_create(ic_pool* pool, const ic_batch_desc* desc, void* dev_w
   if ((uintptr_t)dev_workspace & 255u) return IC_EALIGN;
   std::unique_ptr<ic_plan> pl(new ic_plan());
   if ((rc = plan_within(pool, desc, workspace_bytes, pl->ps)) != IC_OK) return rc;
+  if (!launches_fit(pool, pl->ps)) return IC_EINVAL;
   pl->cfg = pool->cfg;
   pl->tune = pool->tune;
   pl->scale = desc->scale;

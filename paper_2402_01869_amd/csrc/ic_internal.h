@@ -22,7 +22,9 @@ PoolView pool_view(const ic_pool* pool);
 constexpr int kBlockSize = 16;  // tokens per cache block (the only size built)
 // Threads of a launch in one grid dimension: fewer than 2^32.  Of a larger grid the runtime starts the remainder, without an error.
 constexpr uint64_t kMaxLaunchThreads = 0xffffffffull;
-constexpr int kRowWaves = 4;    // waves per workgroup of the row kernel
+constexpr int kRowWaves = 4;    // waves per workgroup of the row kernel,
+constexpr int kGroupWaves = 4;  // ... of the group kernel (whole workgroups per item)
+constexpr int kMergeThreads = 256, kMergeElems = 4 * kMergeThreads;  // values of a row that a workgroup of the merge kernel has
 constexpr int kMaxRowPart = 4096;  // keys per row-kernel work item: 64 block ids per wave
 
 // Query rows per work item of the MFMA tile kernel (planner and kernel must agree).
