@@ -308,10 +308,12 @@ double serial_us(const LaunchRates& rate, double tiles, const RowLoad& r, bool f
   return (few_units ? 17.5 : 24.5) + tiles + std::max(r.bytes / 6.2e6, r.longest / rate.row_alone);
 }
 
-// Row items of an 8-bit pool that a wave has alone, four to a workgroup: whole ones of up to so many keys, once they are more than the places of a
-// workgroup (two to a CU), and of up to twice as many keys once they fill the places of all waves.  A workgroup begins and ends
-// in some 3 us, and on a few keys little else; one that has its place at once is done sooner when its four waves share the keys, and so
-// is the last one (28 rows of 250..500 keys, 40 heads, 23.0 / 24.2).
+// Row items of an 8-bit pool that a wave has alone, four to a workgroup: whole ones of up to so many keys, once they are more than two a CU, and of
+// up to twice as many keys once they are more than eight a CU (head_dim 128 and 256: the places of workgroups and of their waves).  A
+// workgroup begins and ends in some 3 us, and on a few keys little else; one that has its place at once is done sooner when its four waves
+// share the keys, and so is the last one (28 rows of 250..500 keys, 40 heads, 23.0 / 24.2).  At head_dim 64, where a CU has four places, the same
+// numbers of items hold: of 48 batches (224 to 6400 items of 2 to 460 keys) they choose 0.7 % more than the best in the mean (11 % at most),
+// twice as many 1.6 % (17 %).
 // Measured, e4m3, in teams / alone, us: 40 heads, 1 row of 120 keys 4.0 / 5.7, 16 of 250 11.1 / 10.0, 64 of 125..250 29.8 / 24.3, of 250..500 52.2 / 45.1,
 // 256 of 30..60 64.5 / 30.1, of 250..500 173 / 159; 32 heads, 223 of 1..2 40.9 / 14.4; 64 over 8, 256 of 125..250 27.6 / 23.4; 16 of 256 dims, 256 of
 // 60..120 45.9 / 35.3; 8 fresh chunks of 300..800, 64 over 8, whose first 63 rows are such items beside the tiles, 111.6 / 98.2, one of 512, 40 heads (160
@@ -321,16 +323,21 @@ constexpr int kAloneKeys = 256;
 // Workgroups of a row item of an 8-bit pool: K/V heads, times the parts of at most 16 heads of a larger group.
 int q8_row_units(const ic_pool_cfg& c) { return c.num_kv_heads * ((c.num_heads / c.num_kv_heads + 15) / 16); }
 
-// Keys per row item of an 8-bit pool: whole rows (up to kDefaultRowPart keys) once they give every place of a workgroup (two to a CU) two
+// Workgroups of the 8-bit row kernel that a CU has places for.
+constexpr int q8_places(int head_dim) { return head_dim == 64 ? 4 : 2; }
+
+// Keys per row item of an 8-bit pool: whole rows (up to kDefaultRowPart keys) once they give every place of a workgroup two
 // items, before that the partition that is expected to end soonest.  The model, in us: the cached bytes at 6.6 TB/s, or the longest
 // item, which a workgroup alone reads at 27 / 41 / 54 GB/s (head_dim 64 / 128 / 256; integers, whose conversion takes more
 // instructions, 0.85 of that); a little of the longest item's time for the end, where only the longest are left; 2.1 us a round of
-// items; and a split: 1 us, and 0.9 us for every four partitions of the longest row.  Fitted to 34 batches in 11 partitions each
-// (1 to 256 rows of 16 to 8000 keys; rms 8 %); what it chooses takes 4 % longer in the mean than the best (at most 16 %).  Measured per layer (us),
+// items; and a split: 1 us (head_dim 64: 2), and 0.9 us for every four partitions of the longest row.  Fitted to 34 batches in 11 partitions each
+// (1 to 256 rows of 16 to 8000 keys; rms 8 %); what it chooses takes 4 % longer in the mean than the best (at most 16 %).  head_dim 64 by itself, with
+// four places a CU: 208 batches (1 to 256 rows of up to 8000 keys, 1 to 32 K/V heads) in up to 9 partitions, 1.2 % (at most 12 %); with the
+// places and terms of the others 1.9 % (18 %).  Measured per layer (us),
 // chosen partition / whole rows: 13B shape, one row of 3000 keys 10.6 (512) / 23.1; 70B shape, 8 of 1000..8000 24.6 (1024) / 32.6, one of
 // 6000 11.6 (512) / 31.6; GPT-J shape, 2 of 2000 12.9 (512) / 23.9, 16 of 512..2048 33.3 whole, 33.8 in parts of 512.
 int q8_row_part(const ic_pool* pool, const ic_batch_desc* d, const PlanSizes& ps) {
-  const int64_t units = q8_row_units(pool->cfg), slots = 2 * kExpectedCus;
+  const int64_t units = q8_row_units(pool->cfg), slots = q8_places(pool->cfg.head_dim) * kExpectedCus;
   const int D = pool->cfg.head_dim;
   const auto runs_of = [&](int s) -> int64_t {  // row items of sequence s, were they not split
     return route(ps, d->ctx_len[s], d->q_len[s]).rest_rows ? (d->q_len[s] + ps.item_rows - 1) / ps.item_rows : 0;
@@ -346,6 +353,7 @@ int q8_row_part(const ic_pool* pool, const ic_batch_desc* d, const PlanSizes& ps
   if (whole == 0 || whole * units >= 2 * slots) return kDefaultRowPart;
   const double key_bytes = 2.0 * (D + 1);
   const double alone = (D == 64 ? 27e3 : D == 128 ? 41e3 : 54e3) * (pool->cfg.dtype == IC_DTYPE_INT8 ? 0.85 : 1.0);  // bytes per us
+  const double end = D == 64 ? 0.16 : 0.08, split = D == 64 ? 2.0 : 1.0;
   static const int parts[] = {kDefaultRowPart, 2048, 1536, 1024, 768, 512, 384, 256};
   int best = kDefaultRowPart;
   double best_us = 0.0;
@@ -355,8 +363,8 @@ int q8_row_part(const ic_pool* pool, const ic_batch_desc* d, const PlanSizes& ps
     for (int s = 0; s < d->num_seqs; ++s) n += runs_of(s) * ((d->ctx_len[s] + part - 1) / part);
     n *= units;
     const double last = std::min(longest, part) * key_bytes / alone;
-    double us = std::max(last, keys * units * key_bytes / 6.6e6) + (n > slots ? 0.08 : 0.16) * last + 2.1 * n / slots;
-    if (longest > part) us += 1.0 + 0.9 * ((longest + 4 * part - 1) / (4 * part));
+    double us = std::max(last, keys * units * key_bytes / 6.6e6) + (n > slots ? 1.0 : 2.0) * end * last + 2.1 * n / slots;
+    if (longest > part) us += split + 0.9 * ((longest + 4 * part - 1) / (4 * part));
     if (best_us == 0.0 || us < best_us) {
       best = part;
       best_us = us;

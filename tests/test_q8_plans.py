@@ -67,3 +67,16 @@ def test_cache_slots_fit_32_bits(fmt):
     assert e.value.code == B.IC_EINVAL
     cfg = B.make_cfg(most + 1, H, D, dtype=R.FORMATS[fmt])
     assert B.lib().ic_check_batch(C.byref(cfg), C.byref(desc.struct)) == B.IC_EINVAL
+
+
+@FMT
+@pytest.mark.parametrize("H,Hkv", [(32, 32), (64, 16)])
+def test_whole_rows_once_every_place_has_two_items(fmt, H, Hkv):
+    """One long row among short ones stays whole from two items a place on: 2 x 2 x 256 workgroups, at head_dim 64, where a CU has four, twice that."""
+    for D, items in ((64, 2048), (128, 1024), (256, 1024)):
+        for n in (items // Hkv - 1, items // Hkv):
+            ctx = [4000] + [300] * (n - 1)
+            batch = W.assemble_batch(H, D, 16, sum(-(-c // 16) for c in ctx) + 5, ctx, [1] * n, np.random.default_rng(1), num_kv_heads=Hkv)
+            pool = _pool(fmt, batch.pool_blocks, H, D, Hkv)
+            assert (pool.plan_image(B.HostDesc.from_batch(batch))["row_part_tokens"] < 4000) == (n * Hkv < items)
+            pool.close()
