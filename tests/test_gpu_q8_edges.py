@@ -183,3 +183,74 @@ def test_a_weight_ahead_of_the_running_maximum_meets_the_largest_scale(fmt, H, H
     assert np.isfinite(got).all()
     assert (np.abs(got - want) <= (2.0 ** -8 + 1e-5) * np.abs(want) + 1e-3 * dev + 1e-6).all()
     pool.close()
+
+
+def _with_nan_vectors(pool_bytes, batch, H, Hkv, D, which, at, want):
+    """A key (which 0) or a value (1) of K/V head 0 that is not finite at position at[s] of sequence s, and NaN in want where it shows."""
+    codes, scales = R.split(pool_bytes, Hkv, D)
+    for s, t in at.items():
+        b, n, c = batch.block_tables[s, t // 16], int(batch.q_len[s]), int(batch.ctx_len[s])
+        codes[b, which, 0, t % 16] = 0
+        scales[b, 0, which, t % 16] = 255
+        first = max(0, t - (c - n))
+        want[batch.q_start[s] + first:batch.q_start[s] + n, :H // Hkv] = np.nan
+
+
+def _shows_where_it_should(got_bits, want, dev):
+    got, hit = W.bf16_bits_to_f64(got_bits), np.isnan(want)
+    assert np.isnan(got[hit]).all()
+    bound = (2.0 ** -8 + 1e-5) * np.abs(want) + (2.0 ** -8 + 1e-3) * dev + 1e-6
+    assert (np.abs(got - want)[~hit] <= bound[~hit]).all()
+
+
+@FMT
+@pytest.mark.parametrize("H,Hkv,D", [(2, 2, 64), (2, 2, 128), (8, 2, 128), (1, 1, 256)])
+@pytest.mark.parametrize("which", [0, 1])
+@pytest.mark.parametrize("row_launch", [2, 3])
+def test_nan_vectors_in_the_rows_that_run_beside_tiles(fmt, H, Hkv, D, which, row_launch):
+    ctx, q_len = [300, 200, 70, 90, 260], [200, 1, 20, 64, 1]
+    at = {0: 211, 1: 37, 2: 61, 3: 40}                           # (the last sequence has none)
+    rng = np.random.default_rng(6)
+    batch = W.assemble_batch(H, D, 16, 70, ctx, q_len, rng, num_kv_heads=Hkv)
+    pool_bytes = R.random_pool(batch, Hkv, D, fmt, rng)
+    q = W.randn_bf16((sum(q_len), H, D), rng)
+    want, dev = R.attention(pool_bytes, batch, q, Hkv, fmt)
+    _with_nan_vectors(pool_bytes, batch, H, Hkv, D, which, at, want)
+    pool = B.KvPool.from_tensor(torch.from_numpy(pool_bytes).to(DEV), H, D, num_kv_heads=Hkv, dtype=R.FORMATS[fmt])
+    pool.set_tuning(row_launch=row_launch)
+    desc = B.HostDesc.from_batch(batch)
+    qt, out = to_dev_bits(q), torch.zeros(q.shape, dtype=torch.int16, device=DEV)
+    ws = torch.empty(pool.workspace_bytes(desc), dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    pool.paged_attn_mixed(desc, qt.data_ptr(), out.data_ptr(), ws.data_ptr(), ws.numel())
+    torch.cuda.synchronize()
+    _shows_where_it_should(from_dev_bits(out), want, dev)
+    pool.close()
+
+
+@FMT
+@pytest.mark.parametrize("H,Hkv,D", [(8, 8, 64), (8, 8, 128), (3, 3, 256), (24, 2, 128)])
+@pytest.mark.parametrize("which", [0, 1])
+@pytest.mark.parametrize("row_launch", [0, 2, 3])
+def test_nan_vectors_in_rows_that_are_a_wave_each(fmt, H, Hkv, D, which, row_launch):
+    """Short rows in numbers, every fifth with a vector that is not finite, its neighbours in the same workgroup without; fresh and short chunks."""
+    rng = np.random.default_rng(H + D)
+    n = 2 * 2100 // (Hkv * (-(-(H // Hkv) // 16))) // 2 + 3      # more than four times the places
+    ctx = list(rng.integers(1, 70, n)) + [90, 300, 64, 70]
+    q_len = [1] * n + [90, 200, 2, 3]
+    at = {s: int(rng.integers(0, ctx[s])) for s in list(range(0, n, 5)) + [n, n + 2]}
+    batch = W.assemble_batch(H, D, 16, sum(-(-int(c) // 16) for c in ctx) + 5, ctx, q_len, rng, num_kv_heads=Hkv)
+    pool_bytes = R.random_pool(batch, Hkv, D, fmt, rng)
+    q = W.randn_bf16((sum(q_len), H, D), rng)
+    want, dev = R.attention(pool_bytes, batch, q, Hkv, fmt)
+    _with_nan_vectors(pool_bytes, batch, H, Hkv, D, which, at, want)
+    pool = B.KvPool.from_tensor(torch.from_numpy(pool_bytes).to(DEV), H, D, num_kv_heads=Hkv, dtype=R.FORMATS[fmt])
+    pool.set_tuning(row_launch=row_launch)
+    desc = B.HostDesc.from_batch(batch)
+    qt, out = to_dev_bits(q), torch.zeros(q.shape, dtype=torch.int16, device=DEV)
+    ws = torch.empty(pool.workspace_bytes(desc), dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    pool.paged_attn_mixed(desc, qt.data_ptr(), out.data_ptr(), ws.data_ptr(), ws.numel())
+    torch.cuda.synchronize()
+    _shows_where_it_should(from_dev_bits(out), want, dev)
+    pool.close()

@@ -80,3 +80,25 @@ def test_whole_rows_once_every_place_has_two_items(fmt, H, Hkv):
             pool = _pool(fmt, batch.pool_blocks, H, D, Hkv)
             assert (pool.plan_image(B.HostDesc.from_batch(batch))["row_part_tokens"] < 4000) == (n * Hkv < items)
             pool.close()
+
+
+@FMT
+@pytest.mark.parametrize("H,Hkv,D,ctx,q_len", [(8, 8, 128, [3500, 100], [1, 1]), (16, 2, 64, [4000], [1]), (4, 4, 256, [3000, 900], [1, 300])])
+def test_a_workspace_without_room_for_the_splits_is_enough(fmt, H, Hkv, D, ctx, q_len):
+    """A call that gets the bytes of the unsplit plan is planned without the splits; with fewer it is refused.  (No GPU: a call that is not refused
+    fails where it asks for pinned memory.)"""
+    import torch
+    if torch.cuda.device_count() > 0:
+        pytest.skip("the call would run on made-up addresses")
+    batch = W.assemble_batch(H, D, 16, 600, ctx, q_len, np.random.default_rng(1), num_kv_heads=Hkv)
+    pool, desc = _pool(fmt, 600, H, D, Hkv), B.HostDesc.from_batch(batch)
+    full = pool.workspace_bytes(desc)
+    pool.set_tuning(decode_part_tokens=4096, span_part_tokens=1 << 20)
+    least = pool.workspace_bytes(desc)
+    assert pool.plan_query(desc)["partial_slots"] == 0
+    pool.set_tuning()
+    assert pool.plan_query(desc)["partial_slots"] > 0 and least < full
+    at = [0x9000000, 0xa000000, 0xb000000]
+    assert pool.paged_attn_mixed(desc, *at, least, check=False) not in (B.IC_OK, B.IC_ESIZE)
+    assert pool.paged_attn_mixed(desc, *at, least - 256, check=False) == B.IC_ESIZE
+    pool.close()
