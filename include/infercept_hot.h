@@ -174,8 +174,8 @@ int kv_write_span(ic_pool* pool, const ic_batch_desc* desc, const void* dev_k_ne
  * The other way round: reads cached positions back as bf16 rows.  For every sequence s and row i < q_len[s], position
  * t = ctx_len[s] - q_len[s] + i,
  *      k_out|v_out[q_start[s] + i][h][:] = the values at pool[block_tables[s][t / block_size]][K|V][h][t % block_size]
- * q_len = ctx_len reads a whole context (to move it to a pool of another dtype: kv_read_span, then kv_write_span there, which keeps
- * every value of an 8-bit cache).  dev_k_out, dev_v_out: device bf16 [total_q_rows][num_kv_heads][head_dim], not overlapping the pool
+ * q_len = ctx_len reads a whole context (to move it to another pool: kv_read_span, then kv_write_span there.  A pool of bf16 or of the
+ * same 8-bit dtype keeps every value of an 8-bit cache, one of the other 8-bit dtype quantises the values anew).  dev_k_out, dev_v_out: device bf16 [total_q_rows][num_kv_heads][head_dim], not overlapping the pool
  * or each other (IC_EINVAL); rows no sequence owns keep their bytes.  Exact: a bf16 cache's bytes, an 8-bit cache's values.  Sequences
  * may share blocks.
  */

@@ -254,3 +254,31 @@ def test_nan_vectors_in_rows_that_are_a_wave_each(fmt, H, Hkv, D, which, row_lau
     torch.cuda.synchronize()
     _shows_where_it_should(from_dev_bits(out), want, dev)
     pool.close()
+
+
+@FMT
+def test_a_context_moved_to_the_other_dtype_is_quantised_anew(fmt):
+    """The cache there is the definition's of the values here: integers keep less of small numbers than e4m3, e4m3 less of large ones."""
+    H, D = 3, 128
+    other = "int8" if fmt == "e4m3" else "e4m3"
+    rng = np.random.default_rng(15)
+    batch = W.assemble_batch(H, D, 16, 30, [200, 16, 90], [200, 16, 90], rng)
+    desc, src = B.HostDesc.from_batch(batch), R.random_pool(batch, H, D, fmt, rng)
+    a = B.KvPool.from_tensor(torch.from_numpy(src).to(DEV), H, D, dtype=R.FORMATS[fmt])
+    t = torch.from_numpy(R.empty_pool(30, H, D)).to(DEV)
+    b = B.KvPool.from_tensor(t, H, D, dtype=R.FORMATS[other])
+    k, v = (torch.zeros((batch.total_q_rows, H, D), dtype=torch.int16, device=DEV) for _ in range(2))
+    a.kv_read_span(desc, k.data_ptr(), v.data_ptr())
+    b.kv_write_span(desc, k.data_ptr(), v.data_ptr())
+    torch.cuda.synchronize()
+    want = R.empty_pool(30, H, D)
+    _write(want, batch, from_dev_bits(k), from_dev_bits(v), other)
+    got, lost = t.cpu().numpy(), 0
+    for s in range(batch.num_seqs):
+        here = R.context(src, batch, s, H, D, fmt)
+        for x, y, z in zip(here, R.context(got, batch, s, H, D, other), R.context(want, batch, s, H, D, other)):
+            assert np.array_equal(y, z)
+            lost += (x != y).sum()
+    assert lost > 0
+    a.close()
+    b.close()
