@@ -217,7 +217,9 @@ typedef struct {
                                  would leave much of the chip idle)                          */
   int32_t span_kernel;        /* 0 = built-in choice (spans: MFMA tiles; decode rows: vector kernel, or the MFMA
                                  group kernel in a grouped-query pool), 1 = everything row by row on the vector
-                                 kernel, 2 = MFMA tiles, in a grouped-query pool also for decode rows */
+                                 kernel, 2 = MFMA tiles, in a grouped-query pool also for decode rows.  8-bit pools:
+                                 row by row and decode rows are their own row kernel's, on the matrix cores too, and
+                                 0 also leaves it spans of up to three row items (ic_plan_image; head_dim 256: two) */
   int32_t row_variant;        /* vector-kernel build: bit 0 = prefetch two tiles ahead, bit 1 = cached (not non-temporal) KV loads */
   int32_t serial_spans;       /* 1 = run the span kernel, then the row kernel, on the caller's stream; 0 = built-in
                                  choice (large batches, and with row_launch 2 or 3 or row_slots any batch: two
@@ -235,7 +237,8 @@ typedef struct {
                                  bf16 as the matrix-core kernels do (with a handful of keys one weight's rounding
                                  shows in the output): such rows run on the vector kernel, which keeps them in
                                  fp32, or as units that split them into three bf16 parts (24 bits); 0 = built-in 64,
-                                 1 = no such routing, at most 64                              */
+                                 1 = no such routing, at most 64.  8-bit pools: on their row kernel, which keeps
+                                 16 bits of every weight                                      */
   int32_t reserved[1];        /* must be 0                                                   */
 } ic_tuning;
 int ic_pool_set_tuning(ic_pool* pool, const ic_tuning* tuning);

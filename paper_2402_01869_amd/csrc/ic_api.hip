@@ -521,7 +521,8 @@ int choose_row_part_beside(const ic_pool* pool, const ic_batch_desc* d, const Pl
 
 // Time of one 64-key step of a tile workgroup among 256 (1.0 PFLOP/s, head_dim 256: 0.85); it takes the same time however many of
 // the tile's rows are live.  Of 77 batches of chunks, each measured in up to 12 partitions, the ones chosen with it take 0.9 % longer
-// than the best in the mean and 14 % at most (with the 0.9 and 0.5 of the tile kernels before: 1.15 %, 18 %).
+// than the best in the mean and 14 % at most (with the 0.9 and 0.5 of the tile kernels before: 1.15 %, 18 %).  8-bit pools go by the same times,
+// which their kernels were not fitted to: 36 batches of chunks, e4m3 and integers, 2.7 % and 25 % (6 chunks of 690 on 4400, 8 heads).
 double tile_step_us(int head_dim) {
   return 4.0 * tile_rows(head_dim) * 64 * head_dim / ((head_dim > 128 ? 0.85e9 : 1.0e9) / kExpectedCus);
 }

@@ -1,12 +1,14 @@
 // Row kernel of the 8-bit cache: query rows that are few for their keys.  Decode rows of every pool (Section 4.2: one query token,
 // every cached vector read once), short chunks, and the rows of a fresh chunk that see fewer than 64 keys.
 //
-// Measured, GB/s of cached bytes, e4m3 / integers: 128 rows of 256..4096, 40 heads of 128, 6600 / 6560; 256 rows of 512..2048, 16 heads of 256, 6530 / 6560;
-// 128 rows, 32 heads of 64, 6170 / 6020; 64 heads over 8, 5910 / 5450.  Vector ALU 30 % (integers 45 %) and matrix pipe 9 % busy, no LDS
+// Measured, GB/s of cached bytes, e4m3 / integers: 128 rows of 256..4096, 40 heads of 128, 6690 / 6630; 256 rows of 512..2048, 16 heads of 256, 6390 / 6370;
+// 128 rows, 32 heads of 64, 6530 / 6430; 64 heads over 8, 5850 / 5460.  Vector ALU 30 % (integers 45 %) and matrix pipe 9 % busy, no LDS
 // conflicts, 1.02 times the bytes fetched.  Beside the tile kernel, one workgroup a CU, the wait for memory is exposed: 4000 to 5000.
 //
 // One workgroup = one row item (up to 16 columns: consecutive query rows of a sequence x the query heads of a K/V head) x one K/V head,
-// 4 waves, wave w the item's 32-key tiles w, w + 4, ...; of items of few keys that are many, each wave has one (row_long).  HBM-bound: a byte of the cache is read once and meets all columns.
+// 4 waves, wave w the item's 32-key tiles w, w + 4, ...; of items of few keys that are many, each wave has one (row_long).  HBM-bound: a byte of the
+// cache is read once per item and meets all its columns.  The 16-column parts of a larger group, and the items of a span, read it once each: 256 rows of
+// 256..4096 keys, 16 heads over 1 37 us, 24 and 32 over 1 64.
 // Every wave copies its tiles from the pool straight into a ring of its own in LDS (no registers, no barrier), a tile ahead, and codes
 // become MFMA operands in registers:
 //   - S^T = K Q^T (16x16x32): a lane's A operand is 8 numbers of one key.  It reads 16 bytes of the key, two operands; which dims
