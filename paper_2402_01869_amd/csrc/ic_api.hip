@@ -120,7 +120,7 @@ int check_batch(const ic_pool_cfg& cfg, const ic_batch_desc* d, bool trusted) {
   for (int s = 0; s < d->num_seqs; ++s) {
     const int32_t c = d->ctx_len[s], n = d->q_len[s];
     if (c < 1 || n < 1 || n > c) return IC_EINVAL;
-    if ((c + kBlockSize - 1) / kBlockSize > d->max_blocks_per_seq) return IC_ESIZE;
+    if ((c - 1) / kBlockSize >= d->max_blocks_per_seq) return IC_ESIZE;
     const int64_t r0 = d->q_start[s];
     if (r0 < 0 || r0 + n > d->total_q_rows) return IC_EOVERLAP;
     rows += n;

@@ -102,3 +102,12 @@ def test_a_workspace_without_room_for_the_splits_is_enough(fmt, H, Hkv, D, ctx, 
     assert pool.paged_attn_mixed(desc, *at, least, check=False) not in (B.IC_OK, B.IC_ESIZE)
     assert pool.paged_attn_mixed(desc, *at, least - 256, check=False) == B.IC_ESIZE
     pool.close()
+
+
+@pytest.mark.parametrize("dtype", [B.IC_DTYPE_BF16, B.IC_DTYPE_E4M3, B.IC_DTYPE_INT8])
+@pytest.mark.parametrize("ctx", [17, 2 ** 31 - 16, 2 ** 31 - 15, 2 ** 31 - 1])
+def test_a_context_longer_than_its_table(dtype, ctx):
+    """Up to the largest int32, where rounding up to blocks would overflow."""
+    cfg = B.make_cfg(64, 4, 64, dtype=dtype)
+    desc = B.HostDesc([ctx], [1], [0], np.zeros((1, 1), np.int32), 1.0, 1)
+    assert B.lib().ic_check_batch(C.byref(cfg), C.byref(desc.struct)) == B.IC_ESIZE
